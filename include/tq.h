@@ -298,6 +298,122 @@ tq_status tq_export_weights_canonical(const tq_weight_desc *d, const void *packe
 tq_status tq_act_codes_canonical(const void *x_codes, const void *x_scales, int m, int k, int group,
                                  void *codes_out, void *scales_out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Between the linear layers: what a decoder block of a model with quantized
+ * layers computes from its query, key and value projections to the input of its
+ * output projection, for inference.  Values are fp16 or bf16 (tq_dtype).
+ * ------------------------------------------------------------------------- */
+
+/* A paged key-value cache, in the caller's memory.  A slot is one token's place:
+ * slot number = page * page_size + place within the page.
+ *   k, v      [pages, kv_heads, page_size, row], where a row of head_dim values is
+ *               bits 16  the values themselves, of type dtype
+ *               bits  8  head_dim e4m3 codes (OCP fp8, no infinities)
+ *               bits  4  head_dim / 8 TQ4 code words
+ *   k_scales, v_scales  [pages, kv_heads, page_size] fp16, one scale per row (8 and
+ *             4 bits; NULL for 16).  A row stands for code * scale.
+ * The quantizer is that of Sec. 2 Eq. (1) with the row as its group: scale =
+ * fp16(max|x| / 7) and code = clamp(rint(x / scale), -7, 7) at 4 bits, fp16(max|x|
+ * / 448) and x / scale rounded half to even to e4m3 at 8; a row whose scale is
+ * zero has zero codes.
+ * head_dim 64, 128 or 256; page_size a power of two from 16 to 32768; pages *
+ * page_size <= 2^40, kv_heads <= 1024. */
+typedef struct {
+    int32_t pages, page_size, kv_heads, head_dim;
+    int32_t bits, dtype;
+    void *k, *v, *k_scales, *v_scales;
+} tq_kv_cache;
+
+/* 16-bit values [tokens, heads, head_dim] at `data`: strides in values, multiples
+ * of 8 (rows start on 16 bytes), the last axis contiguous.  A view of a fused
+ * projection's output is one. */
+typedef struct {
+    const void *data;
+    int64_t token_stride, head_stride;
+} tq_head_rows;
+
+/* Norm and rotation of query and key rows x of head_dim values, in fp32:
+ *   norm      x / sqrt(mean(x^2) + eps) * weight, weight [head_dim] of the rows'
+ *             type, shared by the heads; left out where the pointer is NULL
+ *   rotation  of the first rotary_dim values (a multiple of 16, at most head_dim;
+ *             0 = none) by the token's row of `table` [max_positions, rotary_dim]
+ *             fp32, rotary_dim / 2 cosines c and then as many sines s:
+ *               halves       (x_i, x_(i + rotary_dim/2)) and, interleaved, pairs
+ *               (x_2i, x_(2i+1)) -> (x c_i - y s_i, y c_i + x s_i)
+ *   positions [tokens] int32, taken into [0, max_positions)
+ * The result is rounded once to 16 bits. */
+typedef struct {
+    const void *q_weight, *k_weight;
+    const int32_t *positions;
+    const float *table;
+    int32_t rotary_dim, max_positions, interleaved;
+    float eps;
+} tq_norm_rope;
+
+/* Query rows [tokens, q_heads, head_dim] and key rows [tokens, kv_heads,
+ * head_dim] normed and rotated, one launch.
+ *   q_out, k_out  of the same shapes, contiguous; either may be the input itself
+ *                 where that is contiguous (a row is read before it is written)
+ * tokens == 0 is a no-op; tokens * (q_heads + kv_heads) < 2^31.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_HIP. */
+tq_status tq_qk_norm_rope(const tq_norm_rope *p, const tq_head_rows *q, const tq_head_rows *k, int tokens,
+                          int q_heads, int kv_heads, int head_dim, tq_dtype dtype, void *q_out, void *k_out,
+                          void *stream);
+
+/* Key and value rows [tokens, kv_heads, head_dim] into the cache, one launch.
+ *   slots  [tokens] int64; a token whose slot is negative or past the cache is not
+ *          written; slots of one call are distinct (a slot given twice holds
+ *          either token's row)
+ * With 16 bits dtype is the cache's.  tokens == 0 is a no-op; 2 * tokens *
+ * kv_heads < 2^31.  Errors as above, TQ_ERR_BUFFER for a cache with unsupported
+ * sizes. */
+tq_status tq_kv_append(const tq_kv_cache *c, const tq_head_rows *k, const tq_head_rows *v,
+                       const int64_t *slots, int tokens, tq_dtype dtype, void *stream);
+
+/* Both of the above in one launch: query rows to q_out, key rows normed, rotated
+ * and rounded as in tq_qk_norm_rope, then key and value rows into the cache as in
+ * tq_kv_append (the same bits).  k_out may be NULL. */
+tq_status tq_qk_norm_rope_append(const tq_norm_rope *p, const tq_kv_cache *c, const tq_head_rows *q,
+                                 const tq_head_rows *k, const tq_head_rows *v, const int64_t *slots,
+                                 int tokens, int q_heads, tq_dtype dtype, void *q_out, void *k_out,
+                                 void *stream);
+
+/* Rows of slots [tokens] int64 out of the cache, as values of type dtype (code *
+ * scale in fp32, rounded once; the cache's type with 16 bits) in k_out and v_out
+ * [tokens, kv_heads, head_dim].  A slot outside the cache gives zeros.  Errors as
+ * tq_kv_append. */
+tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, void *k_out, void *v_out,
+                     tq_dtype dtype, void *stream);
+
+/* Attention of one new token of every stream over the cache:
+ *   out[i, h] = sum_t w_t v_t,  w = softmax over t of scale * (q[i, h] . k_t),
+ * for the tokens t in [max(0, lengths[i] - window), lengths[i]) of stream i (window
+ * 0: from 0), with key-value head h / (q_heads / kv_heads).
+ *   q           [batch, q_heads, head_dim] of type dtype
+ *   page_table  [batch] rows of max_pages page numbers, table_stride apart: token t
+ *               of stream i is in page page_table[i][t / page_size].  Pages before
+ *               the window's and past the length's are not looked up; a number
+ *               outside the cache is taken to its nearest page
+ *   lengths     [batch] int32, taken into [0, max_pages * page_size].  A stream of
+ *               length 0 gives zeros
+ *   out         [batch, q_heads, head_dim] of type dtype
+ *   lse         [batch, q_heads] fp32, the natural logarithm of the sum of
+ *               exp(scale * q . k) (-infinity for length 0), or NULL
+ *   scratch     device buffer of tq_paged_attention_scratch_bytes bytes, 16-byte
+ *               aligned, free again when the stream has run the call
+ * What slots outside a stream's range hold (NaN too) has no effect.  Scores, the
+ * softmax and the sums are fp32; its weights enter the products with v with 11
+ * bits (fp16 cache) or 16 (the others).  Two launches; the result does not depend
+ * on timing.  batch == 0 is a no-op; batch <= 65535, max_pages * page_size <= 2^30,
+ * q_heads a multiple of kv_heads, at most 65535.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_BUFFER,
+ * TQ_ERR_HIP; the scratch size is 0 for arguments that would be refused. */
+size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int max_pages);
+tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
+                             int q_heads, const int32_t *page_table, int64_t table_stride, int max_pages,
+                             const int32_t *lengths, float scale, int window, void *out, float *lse,
+                             void *scratch, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *tq_status_string(tq_status s);
 

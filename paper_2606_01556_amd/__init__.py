@@ -45,7 +45,8 @@ EXPORTS = ("tq_weight_desc_init", "tq_pack_weights", "tq_quant_act", "tq_dual_ge
            "tq_act_codes_bytes", "tq_unfused_scratch_bytes", "tq_dual_gemm_unfused",
            "tq_dual_gemm_unfused_noalloc", "tq_dual_gemm_kernel", "tq_dual_gemm_block", "tq_status_string",
            "tq_export_weights_canonical", "tq_act_codes_canonical", "tq_layer",
-           "tq_layer_scratch_bytes")
+           "tq_layer_scratch_bytes", "tq_qk_norm_rope", "tq_kv_append", "tq_qk_norm_rope_append", "tq_kv_read",
+           "tq_paged_attention_scratch_bytes", "tq_paged_attention")
 
 _lib = None
 
@@ -83,8 +84,9 @@ def lib() -> ctypes.CDLL:
         L.tq_act_codes_canonical.argtypes = [P, P, I, I, I, P, P, P]
         L.tq_status_string.argtypes = [I]
         L.tq_status_string.restype = ctypes.c_char_p
+        kvcache.declare(L)
         for name in EXPORTS:
-            if name not in ("tq_act_codes_bytes", "tq_unfused_scratch_bytes", "tq_layer_scratch_bytes",
+            if name not in ("tq_act_codes_bytes", "tq_paged_attention_scratch_bytes", "tq_unfused_scratch_bytes", "tq_layer_scratch_bytes",
                             "tq_dual_gemm_kernel", "tq_status_string"):
                 getattr(L, name).restype = I
         _lib = L
@@ -530,3 +532,8 @@ def act_codes_rows(x_codes, m: int) -> np.ndarray:
     b = w.view(np.uint8).reshape(tiles, kg, 2, 2, 32, 16)   # tile, group, part, half, token, byte
     b = b.transpose(0, 4, 1, 3, 2, 5)                        # tile, token, group, half, part, byte
     return fp8_code_decode(b.reshape(tiles * 32, kg * 64))[:m]
+
+
+from . import kvcache                                                          # noqa: E402
+from .kvcache import (KVCache, empty_kv_cache, kv_append, kv_read, paged_attention,   # noqa: E402,F401
+                      qk_norm_rope, qk_norm_rope_append, rope_table)
