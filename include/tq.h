@@ -400,15 +400,18 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
  *   lse         [batch, q_heads] fp32, the natural logarithm of the sum of
  *               exp(scale * q . k) (-infinity for length 0), or NULL
  *   scratch     device buffer of tq_paged_attention_scratch_bytes bytes, 16-byte
- *               aligned, free again when the stream has run the call
+ *               aligned, free again when the stream has run the call; may be NULL
+ *               where that size is 0 (short streams)
  * What slots outside a stream's range hold (NaN too) has no effect.  Scores, the
- * softmax and the sums are fp32; its weights enter the products with v with 11
- * bits (fp16 cache) or 16 (the others).  Two launches; the result does not depend
- * on timing.  batch == 0 is a no-op; batch <= 65535, max_pages * page_size <= 2^30,
- * q_heads a multiple of kv_heads, at most 65535.
+ * softmax and the sums are fp32; the softmax's weights enter the products with v
+ * with 16 bits or more.  One launch for short streams, else two; the result does not
+ * depend on timing.  batch == 0 is a no-op; batch <= 65535, max_pages
+ * * page_size <= 2^30, q_heads a multiple of kv_heads, at most 65535; all streams' and
+ * heads' tokens, as the page table bounds them, in units of 32 below 2^31 - 2^16.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_BUFFER,
  * TQ_ERR_HIP; the scratch size is 0 for arguments that would be refused. */
-size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int max_pages);
+size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int max_pages,
+                                        int window);
 tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
                              int q_heads, const int32_t *page_table, int64_t table_stride, int max_pages,
                              const int32_t *lengths, float scale, int window, void *out, float *lse,

@@ -6,26 +6,34 @@
 // group), so the kernel is built around one pass over them with nothing but
 // registers between memory and the matrix cores:
 //
-//  * S^T = K Q^T in 16x16x32 products.  A lane of the first operand holds eight
-//    values of one token's key, which is a run of the cache row as it lies in
-//    memory; the group's query heads (up to 16) are the columns.  Which of a
-//    row's values make up one product is free as long as Q is laid out alike, so
-//    each format loads the widest run a lane can.
+//  * S^T = K Q^T with the group's query heads (up to 16) as columns.  A lane of the
+//    first operand holds values of one token's key, a run of the cache row as it
+//    lies in memory: which of a row's values make up one product is free as long as
+//    Q is laid out alike, so each format loads the widest run a lane can.  16-bit
+//    rows enter 16x16x32 products as they are.  Codes (d >= 128) enter 16x16x128
+//    products as e4m3 bytes, also as they are: Q is split into e4m3 terms instead,
+//    each 2^-4 of the one before, three for fp16 and two for bf16, which hold its
+//    significand exactly.
 //  * The result has column lane % 16 and rows 4 (lane / 16) + i: a lane holds the
 //    scores of one head for tokens 4 g + i.  Two such tiles, exponentiated, are
 //    the second operand of O^T = V^T P^T as they stand (the order of the tokens
 //    is free too), so no score crosses lanes.
 //  * V^T's operand takes eight tokens' values of one channel per lane.  A lane
 //    loads rows 4 g + i of the tile, channels DV r .. DV r + DV - 1 (r = lane %
-//    16, DV = d / 16), and pairs the rows up with byte permutes.
-//  * The running maximum is a reference only: it moves when some score passes it
-//    by 2^8, so that most steps have no exchange between lanes and no rescaling.
+//    16, DV = d / 16), and pairs the rows up with byte permutes.  The scale of a
+//    quantized row is part of its weight.
+//  * The softmax's reference (and with it the scaling of the weights) only moves
+//    when some weight passes 2^8: most steps have no exchange between lanes and no
+//    rescaling.  Weights in fp16 then keep 11 bits down to 2^-22 of the largest.
 //
-// The work is cut evenly whatever the lengths: all (stream, head) ranges of
-// units laid end to end are split into equal runs, one per work-group.  A range
-// that one run holds whole is written at once; the ends of the others are joined
-// by a second launch, in order, so a result does not depend on timing.
+// The work is cut evenly whatever the lengths: all (stream, head) ranges of steps
+// laid end to end are split into equal runs, one per work-group, and a work-group's
+// eight wavefronts take its steps in turn.  A range that one run holds whole is
+// written at once; a second launch joins the parts of the others, in their order, so
+// that a result does not depend on timing.  Short ranges get a work-group each and
+// need no second launch.
 #include "tq_device.hpp"
+#include "tq_kernels.hpp"
 #include "tq_kv.hpp"
 
 namespace tq {
@@ -37,14 +45,17 @@ typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef const int32_t __attribute__((address_space(4))) const_i32;
 
-constexpr int kWaves = 4;
 constexpr int kHeads = 16;                 // query heads per work-group (columns of a product)
+constexpr int kRunWaves = 4;               // wavefronts of a work-group that holds a run of steps,
+constexpr int kMostRuns = 2 * 256;         // two such per CU
+constexpr int kDirectWaves = 8;            // ... that holds one short range
+constexpr int kJoinThreads = 256;
 
-// tokens a wavefront takes at a time, and a work-group's unit
-constexpr int step_tokens(int bits) { return bits == 16 ? 32 : 64; }
-constexpr int unit_tokens(int bits) { return kWaves * step_tokens(bits); }
+// tokens of one step of a wavefront
+constexpr int step_tokens(int d, int bits) { return d * bits >= 1024 ? 32 : 64; }
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -75,104 +86,138 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
   if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
 }
+// the two values of such a word
+template <bool BF16>
+__device__ __forceinline__ f2 unpack2(uint32_t w) {
+  if constexpr (BF16) return f2{__builtin_bit_cast(float, w << 16), __builtin_bit_cast(float, w & 0xffff0000u)};
+  else return __builtin_convertvector(__builtin_bit_cast(h2, w), f2);
+}
 
-// NB bytes from p (p aligned to min(NB, 16))
+// NB bytes from p (p aligned to min(NB, 16)).  The cache is read once per call:
+// non-temporal loads stream it at 7.0 TB/s instead of 6.2 (512 MB).
+template <typename T>
+__device__ __forceinline__ T stream_load(const uint8_t *p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
+}
 template <int NB>
 __device__ __forceinline__ void load_bytes(const uint8_t *p, uint32_t *out) {
   if constexpr (NB >= 16) {
 #pragma unroll
     for (int i = 0; i < NB / 16; i++) {
-      const u32x4 v = *reinterpret_cast<const u32x4 *>(p + 16 * i);
+      const u32x4 v = stream_load<u32x4>(p + 16 * i);
       out[4 * i] = v.x; out[4 * i + 1] = v.y; out[4 * i + 2] = v.z; out[4 * i + 3] = v.w;
     }
   } else if constexpr (NB == 8) {
-    const uint2 v = *reinterpret_cast<const uint2 *>(p);
+    const u32x2 v = stream_load<u32x2>(p);
     out[0] = v.x; out[1] = v.y;
   } else {
     static_assert(NB == 4);
-    out[0] = *reinterpret_cast<const uint32_t *>(p);
+    out[0] = stream_load<uint32_t>(p);
   }
 }
 
-// Units of a stream: [first, len) in units from first rounded down to 16.
+// fp16 scale j of four
+__device__ __forceinline__ float scale_of(u32x2 four, int j) {
+  const uint32_t two = j < 2 ? four.x : four.y;
+  return (float)__builtin_bit_cast(h2, two)[j & 1];
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The tokens [first, len) of a stream in steps from first rounded down to 16.
 struct Range {
-  int first, len, base, units;
+  int first, len, base, steps;
 };
-template <int UT>
+template <int ST>
 __device__ __forceinline__ Range range_of(int len, int cap, int window) {
   Range r;
   r.len = min(max(len, 0), cap);
   r.first = window > 0 && r.len > window ? r.len - window : 0;
   r.base = r.first & ~15;
-  r.units = (r.len - r.base + UT - 1) / UT;
+  r.steps = (r.len - r.base + ST - 1) / ST;
   return r;
 }
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-// Sum of units of streams [0, until) in every lane of the wavefront.
-template <int UT>
-__device__ int units_before(const AttendArgs &a, int cap, int until) {
-  int s = 0;
-  for (int b = threadIdx.x & 63; b < until; b += 64) s += range_of<UT>(a.lengths[b], cap, a.window).units;
+// steps of streams b0 + lane, summed over the lanes up to this one
+template <int ST>
+__device__ __forceinline__ int scan64(const AttendArgs &a, int cap, int b0) {
+  const int lane = threadIdx.x & 63, b = b0 + lane;
+  int incl = b < a.batch ? range_of<ST>(a.lengths[b], cap, a.window).steps : 0;
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
-  return uniform(s);
-}
-
-// The stream that holds unit x of all streams' units laid end to end, and the
-// units before it (x below the total).
-template <int UT>
-__device__ void locate(const AttendArgs &a, int cap, int x, int &stream, int &before) {
-  const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += 64) {
-    const int b = b0 + lane;
-    int incl = b < a.batch ? range_of<UT>(a.lengths[b], cap, a.window).units : 0;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const int o = __shfl_up(incl, m);
-      if (lane >= m) incl += o;
-    }
-    const uint64_t past = __ballot(sum + incl > x);
-    if (past != 0) {
-      const int at = __builtin_ctzll(past);
-      stream = b0 + at;
-      before = sum + (at == 0 ? 0 : uniform(__shfl(incl, at - 1)));
-      stream = uniform(stream);
-      before = uniform(before);
-      return;
-    }
-    sum += uniform(__shfl(incl, 63));
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(incl, m);
+    if (lane >= m) incl += o;
   }
-  stream = a.batch;
-  before = sum;
+  return incl;
 }
 
-// floats of one partial result: the group's maxima and sums, then its products
-__host__ __device__ constexpr int partial_head(int cols) { return (2 * cols + 3) & ~3; }
-__host__ __device__ constexpr int partial_floats(int d, int cols) { return partial_head(cols) + cols * d; }
+// How the call's steps are cut: run w holds steps [w chunk, (w + 1) chunk) of all
+// ranges laid end to end, of every stream's `vheads` ranges in turn.
+struct Cut {
+  int total, chunk;
+};
+template <int ST>
+__device__ Cut cut_of(const AttendArgs &a, int cap, int vheads, int runs, int &first64) {
+  Cut c;
+  first64 = scan64<ST>(a, cap, 0);
+  int sum = uniform(__shfl(first64, 63));
+  for (int b0 = 64; b0 < a.batch; b0 += 64) sum += uniform(__shfl(scan64<ST>(a, cap, b0), 63));
+  c.total = sum * vheads;                       // < 2^31 (host)
+  c.chunk = max((c.total + runs - 1) / runs, kRunWaves);
+  return c;
+}
+
+// floats of one part of a range: the group's references and sums, then its products
+__host__ __device__ constexpr int part_head(int cols) { return (2 * cols + 3) & ~3; }
+__host__ __device__ constexpr int part_floats(int d, int cols) { return part_head(cols) + cols * d; }
+
+// Q in LDS instead of registers, which 16-bit rows of 256 values leave none for
+constexpr bool q_in_lds(int d, int bits) { return d == 256 && bits == 16; }
+
+// floats of LDS: [W][kHeads] references and sums, Q where it is there, then [W][cols]
+// [d + 4] products (rows staggered over the banks)
+constexpr int lds_floats(int waves, int d, int bits, int cols) {
+  return 2 * waves * kHeads + (q_in_lds(d, bits) ? d / 32 * 64 * 4 : 0) + waves * cols * (d + 4);
+}
+
+// a head's four output values from d0, and its log-sum-exp
+template <bool BF16>
+__device__ __forceinline__ void store4(const AttendArgs &a, int d, int64_t row, int d0, float m, float l, v4f o) {
+  const float inv = 1.0f / l;
+  *reinterpret_cast<u32x2 *>(a.out + row * d + d0) = u32x2{pack2<BF16>(o[0] * inv, o[1] * inv), pack2<BF16>(o[2] * inv, o[3] * inv)};
+  if (a.lse != nullptr && d0 == 0) a.lse[row] = (m + log2f(l)) * (1.0f / kLog2e);
+}
+
+// What the first launch tells the join about a range, [batch][vheads]: the number
+// of its first part and of its parts (0: nothing to join).  Part 2 w is the first
+// that run w holds, 2 w + 1 the last one if that is another; so the parts of a range
+// are its first, and the first ones of the runs behind it.
+struct Join {
+  int first, parts;
+};
 
 // ---------------------------------------------------------------------------
-template <int D, int BITS, bool BF16>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a) {
-  constexpr int ST = step_tokens(BITS), UT = unit_tokens(BITS), NT = ST / 16;
-  constexpr int RB = D * BITS / 8;            // bytes of a row
+template <int W, int D, int BITS, bool BF16>
+__global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
+  constexpr bool DIRECT = W == kDirectWaves;   // one range per work-group
+  constexpr int ST = step_tokens(D, BITS), NT = ST / 16;
+  constexpr uint32_t RB = D * BITS / 8;       // bytes of a row
   constexpr int CE = BITS == 16 ? 8 : BITS == 8 ? 16 : (D / 4 < 32 ? D / 4 : 32);  // a lane's run of a key row
-  constexpr int CB = CE * BITS / 8;           // its bytes
+  constexpr uint32_t CB = CE * BITS / 8;      // its bytes
   constexpr int KL = D / (4 * CE);            // runs per lane
-  constexpr int KW = KL * CB / 4;             // words
+  constexpr int KW = KL * (int)CB / 4;        // words
   constexpr int KS = D / 32;                  // products per tile of keys
   constexpr int DV = D / 16;                  // channels per lane of a value row
-  constexpr int VBr = DV * BITS / 8;          // their bytes; two lanes share a word of 4-bit codes at d = 64
-  constexpr int VB = VBr < 4 ? 4 : VBr;
-  constexpr int VW = VB / 4;
-  constexpr bool VBF = BITS == 16 ? BF16 : true;   // type of the second product
-  constexpr bool SPLIT = VBF;                 // its weights in two parts (bf16 has 8 bits)
-  constexpr int LD = D + 4;                   // LDS row of one head, staggered over the banks
+  constexpr uint32_t VBr = DV * BITS / 8;     // their bytes; two lanes share a word of 4-bit codes at d = 64
+  constexpr uint32_t VB = VBr < 4 ? 4 : VBr;
+  constexpr int VW = (int)VB / 4;
+  constexpr bool VBF = BITS == 16 && BF16;    // type of the second product: bf16, else fp16
+  constexpr int LD = D + 4;
+  constexpr bool QL = q_in_lds(D, BITS);
 
-  __shared__ float lds_o[kWaves][kHeads][LD];
-  __shared__ float lds_m[kWaves][kHeads], lds_l[kWaves][kHeads];
+  extern __shared__ __attribute__((aligned(16))) float lds[];
+  float *const lds_m = lds, *const lds_l = lds + W * kHeads, *const lds_q = lds + 2 * W * kHeads,
+               *const lds_o = lds_q + (QL ? KS * 64 * 4 : 0);
 
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -181,68 +226,140 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a)
   const int hblocks = (a.group + kHeads - 1) / kHeads, vheads = hkv * hblocks;
   const int cols = min(a.group, kHeads);
 
-  // this work-group's run of units
-  const int per_head = units_before<UT>(a, cap, a.batch);
-  const int64_t total = (int64_t)per_head * vheads;
-  const int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
-  const int64_t x0 = blockIdx.x * chunk, x1 = min(total, x0 + chunk);
+  // this work-group's run of steps
+  int b, vh, t, x0, x1, chunk;
+  Range rg = {};
+  if constexpr (DIRECT) {
+    b = blockIdx.x / vheads;
+    vh = blockIdx.x % vheads;
+    rg = range_of<ST>(uniform(a.lengths[b]), cap, a.window);
+    t = x0 = 0;
+    x1 = chunk = rg.steps;
+  } else {
+    int first64;
+    const Cut cut = cut_of<ST>(a, cap, vheads, gridDim.x, first64);
+    chunk = cut.chunk;
+    x0 = blockIdx.x * chunk;
+    x1 = min(cut.total, x0 + chunk);
+    b = 0;
+    vh = t = 0;
+    if (x0 < x1) {
+      // the stream that holds step x0: the first whose steps end past it
+      const int y = x0 / vheads;
+      int before = 0, incl = first64, b0 = 0;
+      uint64_t past;
+      while ((past = __ballot(before + incl > y)) == 0) {
+        before += uniform(__shfl(incl, 63));
+        b0 += 64;
+        incl = scan64<ST>(a, cap, b0);
+      }
+      const int at = __builtin_ctzll(past);
+      b = uniform(b0 + at);
+      before += at == 0 ? 0 : uniform(__shfl(incl, at - 1));
+      rg = range_of<ST>(uniform(a.lengths[b]), cap, a.window);
+      vh = (x0 - before * vheads) / rg.steps;
+      t = (x0 - before * vheads) % rg.steps;
+    }
+  }
+  float *const parts = a.scratch;
+  Join *const joins = reinterpret_cast<Join *>(a.scratch + (int64_t)gridDim.x * 2 * part_floats(D, cols));
+  // streams that hold nothing
+  auto clear = [&](int64_t row0, int rows) {
+    for (int e = threadIdx.x; e < rows * (D / 2); e += 64 * W) reinterpret_cast<uint32_t *>(a.out + row0 * D)[e] = 0;
+    if (a.lse != nullptr)
+      for (int e = threadIdx.x; e < rows; e += 64 * W) a.lse[row0 + e] = -INFINITY;
+  };
+  if constexpr (DIRECT) {
+    const int h0 = vh % hblocks * kHeads;
+    if (x1 == 0) clear((int64_t)b * a.hq + vh / hblocks * a.group + h0, min(kHeads, a.group - h0));
+  } else {
+    for (int i = blockIdx.x; i < a.batch; i += gridDim.x)
+      if (range_of<ST>(uniform(a.lengths[i]), cap, a.window).steps == 0) {
+        clear((int64_t)i * a.hq, a.hq);
+        for (int e = threadIdx.x; e < vheads; e += 64 * W) joins[(int64_t)i * vheads + e] = Join{0, 0};
+      }
+  }
   if (x0 >= x1) return;
-  int b, before;
-  locate<UT>(a, cap, (int)(x0 / vheads), b, before);
-  Range rg = range_of<UT>(uniform(a.lengths[b]), cap, a.window);
-  int vh = (int)((x0 - (int64_t)before * vheads) / rg.units);
-  int t = (int)((x0 - (int64_t)before * vheads) % rg.units);
-  const float c1 = a.scale * kLog2e;
-  float *part = a.scratch + (int64_t)blockIdx.x * 2 * partial_floats(D, cols);
+  // a wavefront that is behind goes first: wavefronts that progress alike end together
+  // (oldest first, the younger ones are left to themselves at the end)
+  __builtin_amdgcn_s_setprio(3);
+  const int quarter = max((x1 - x0) / 4, 1);
 
-  for (int64_t x = x0; x < x1;) {
-    const int n = (int)min((int64_t)(rg.units - t), x1 - x);
+  for (int x = x0; x < x1;) {
+    const int n = min(rg.steps - t, x1 - x);
     const int kvh = vh / hblocks, hb = vh % hblocks;
     const int heads = min(kHeads, a.group - hb * kHeads);   // live columns
 
-    // Q^T: column r, the values of the runs a key lane loads
+    const_i32 *pages = (const_i32 *)(a.table + b * a.table_stride);
+    const int last_page = (rg.len - 1) >> lps;
+    uint32_t kraw[NT][KW], vraw[NT][4][VW];
+    u32x2 ksr[NT], vsr[NT];
+    // the page of the tile at token tt (a tile past the end takes the last page and is masked)
+    auto page_of = [&](int tt) -> int { return pages[min(tt >> lps, last_page)]; };
+    // row of the cache sections at which the tile starts
+    auto row_of = [&](int page, int tt) -> int64_t {
+      page = min(max(page, 0), a.c.pages - 1);
+      return (((int64_t)page * hkv + kvh) << lps) + (tt & ((1 << lps) - 1));
+    };
+    const uint32_t kofs = r * RB + g * CB, vofs = 4 * g * RB + (VBr < 4 ? (r >> 1) * 4 : r * VB), sofs = 8 * g;
+    auto load_k = [&](const int64_t (&row)[NT]) {
+#pragma unroll
+      for (int i = 0; i < NT; i++) {
+        const uint8_t *kp = a.c.k + row[i] * RB;
+#pragma unroll
+        for (int j = 0; j < KL; j++) load_bytes<CB>(kp + j * 4 * CB + kofs, &kraw[i][j * (int)CB / 4]);
+        if constexpr (BITS < 16)
+          ksr[i] = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const uint8_t *>(a.c.ks + row[i]) + sofs);
+      }
+    };
+    auto load_v = [&](const int64_t (&row)[NT]) {
+#pragma unroll
+      for (int i = 0; i < NT; i++)
+        if constexpr (BITS < 16)
+          vsr[i] = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const uint8_t *>(a.c.vs + row[i]) + sofs);
+#pragma unroll
+      for (int i = 0; i < NT; i++) {
+        const uint8_t *vp = a.c.v + row[i] * RB;
+#pragma unroll
+        for (int j = 0; j < 4; j++) load_bytes<VB>(vp + j * RB + vofs, vraw[i][j]);
+      }
+    };
+
+    // the wavefront's steps t + w, t + w + W, ... of the range
+    int t0 = uniform(rg.base + (t + w) * ST);
+    const int steps = (n - w + W - 1) / W;
+    int64_t row[NT];
+    if (steps > 0) {
+#pragma unroll
+      for (int i = 0; i < NT; i++) row[i] = row_of(page_of(t0 + 16 * i), t0 + 16 * i);
+      load_k(row);
+      load_v(row);
+    }
+
+    // Q^T: column r, the values of the runs a key lane loads; c1: what a score's
+    // product with the key's scale is multiplied by, log2(e) |scale| (its sign goes to Q)
     u32x4 q[KS];
+    const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);     // (-infinity times it has to stay so)
     {
       const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + hb * kHeads + min(r, heads - 1)) * a.q_hs;
+      const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, live = r < heads ? 0xffffffffu : 0u;
 #pragma unroll
-      for (int s = 0; s < KS; s++) {
-        const int d0 = (8 * s / CE) * 4 * CE + g * CE + 8 * s % CE;
-        q[s] = *reinterpret_cast<const u32x4 *>(qp + d0);
-        if (r >= heads) q[s] = u32x4{0, 0, 0, 0};
+      for (int k = 0; k < KS; k++) {
+        if (QL && k % W != w) continue;
+        q[k] = *reinterpret_cast<const u32x4 *>(qp + (8 * k / CE) * 4 * CE + g * CE + 8 * k % CE);
+#pragma unroll
+        for (int i = 0; i < 4; i++) q[k][i] = (q[k][i] ^ flip) & live;
+        if constexpr (QL) *reinterpret_cast<u32x4 *>(lds_q + (k * 64 + lane) * 4) = q[k];
       }
+      if constexpr (QL) __syncthreads();
     }
     v4f o[DV];
 #pragma unroll
     for (int i = 0; i < DV; i++) o[i] = v4f{0, 0, 0, 0};
     float m = -INFINITY, l = 0.0f;
-
-    const_i32 *pages = (const_i32 *)(a.table + b * a.table_stride);
-    const int last_page = (rg.len - 1) >> lps;
-    for (int u = t; u < t + n; u++) {
-      const int t0 = uniform(rg.base + u * UT + w * ST);
-      if (t0 >= rg.len) break;
-      uint32_t kraw[NT][KW], vraw[NT][4][VW];
-      uint2 ksr[NT], vsr[NT];
-#pragma unroll
-      for (int i = 0; i < NT; i++) {
-        const int tt = t0 + 16 * i;
-        // (a tile past the end reads the last page and is masked)
-        int page = pages[min(tt >> lps, last_page)];
-        page = min(max(page, 0), a.c.pages - 1);
-        const int64_t row = (((int64_t)page * hkv + kvh) << lps) + (tt & ((1 << lps) - 1));
-        const uint8_t *kp = a.c.k + row * RB, *vp = a.c.v + row * RB;
-#pragma unroll
-        for (int j = 0; j < KL; j++) load_bytes<CB>(kp + r * RB + j * 4 * CB + g * CB, &kraw[i][j * CB / 4]);
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-          load_bytes<VB>(vp + (4 * g + j) * RB + (VBr < 4 ? (r >> 1) * 4 : r * VB), vraw[i][j]);
-        if constexpr (BITS < 16) {
-          ksr[i] = *reinterpret_cast<const uint2 *>(a.c.ks + row + 4 * g);
-          vsr[i] = *reinterpret_cast<const uint2 *>(a.c.vs + row + 4 * g);
-        }
-      }
-      // scores: row 4 g + j of tile i, head r, times log2 e
-      float s[NT][4];
+    float s[NT][4];
+    // scores, times the keys' scales: row 4 g + j of tile i, head r
+    auto scores = [&]() {
 #pragma unroll
       for (int i = 0; i < NT; i++) {
         v4f acc = {0, 0, 0, 0};
@@ -252,89 +369,109 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a)
           if constexpr (BITS == 16) {
             op = u32x4{kraw[i][4 * k], kraw[i][4 * k + 1], kraw[i][4 * k + 2], kraw[i][4 * k + 3]};
           } else {
-            uint32_t w0, w1, x0_, x1_, x2_, x3_;
+            uint32_t w0, w1, y0, y1, y2, y3;
             if constexpr (BITS == 8) {
               w0 = kraw[i][2 * k];
               w1 = kraw[i][2 * k + 1];
             } else {
               tq4_to_fp8(kraw[i][k], w0, w1);
             }
-            const float sc = BITS == 4 ? 512.0f : 1.0f;
-            widen4<BF16>(w0, sc, x0_, x1_);
-            widen4<BF16>(w1, sc, x2_, x3_);
-            op = u32x4{x0_, x1_, x2_, x3_};
+            widen4<BF16>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+            widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+            op = u32x4{y0, y1, y2, y3};
           }
-          acc = mfma16<BF16>(op, q[k], acc);
+          acc = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + (k * 64 + lane) * 4) : q[k], acc);
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-          float c = c1;
-          if constexpr (BITS < 16) {
-            const uint32_t sw = j < 2 ? ksr[i].x : ksr[i].y;
-            c *= half_bits_to_float((uint16_t)(j & 1 ? sw >> 16 : sw & 0xffffu));
-          }
-          s[i][j] = acc[j] * c;
-        }
+        for (int j = 0; j < 4; j++) s[i][j] = BITS < 16 ? fmaf(acc[j], scale_of(ksr[i], j), 0.0f) : acc[j];
       }
-      float vs[NT][4];
-      if constexpr (BITS < 16) {
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const uint32_t sw = j < 2 ? vsr[i].x : vsr[i].y;
-            vs[i][j] = half_bits_to_float((uint16_t)(j & 1 ? sw >> 16 : sw & 0xffffu));
-          }
-      }
-      if (t0 < rg.first || t0 + ST > rg.len) {
-        // tokens outside the range: no score, and nothing of what their rows hold
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const int tok = t0 + 16 * i + 4 * g + j;
-            const bool in = tok >= rg.first && tok < rg.len;
-            s[i][j] = in ? s[i][j] : -INFINITY;
-            if constexpr (BITS < 16) vs[i][j] = in ? vs[i][j] : 0.0f;
-#pragma unroll
-            for (int k = 0; k < VW; k++) vraw[i][j][k] = in ? vraw[i][j][k] : 0u;
-          }
-      }
-      float top = s[0][0];
+    };
+    // tokens outside the range: no score, and nothing of what their rows hold
+    auto masked = [&](int i, int j) -> bool {
+      const int tok = t0 + 16 * i + 4 * g + j;
+      return tok < rg.first || tok >= rg.len;
+    };
+    auto mask_scores = [&]() {
+      asm volatile("");          // (a branch: selects in every step would cost a fifth of it)
 #pragma unroll
       for (int i = 0; i < NT; i++)
 #pragma unroll
-        for (int j = 0; j < 4; j++) top = fmaxf(top, s[i][j]);
-      if (__any(top > m + 8.0f)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float m1 = fmaxf(m, top);
+        for (int j = 0; j < 4; j++) {
+          s[i][j] = masked(i, j) ? -INFINITY : s[i][j];
+          if constexpr (BITS < 16) vsr[i][j / 2] &= masked(i, j) ? (j & 1 ? 0x0000ffffu : 0xffff0000u) : 0xffffffffu;
+        }
+    };
+    auto mask_values = [&]() {
+      asm volatile("");
+#pragma unroll
+      for (int i = 0; i < NT; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+          for (int k = 0; k < VW; k++) vraw[i][j][k] = masked(i, j) ? 0u : vraw[i][j][k];
+    };
+    // weights p in s, times the values' scales
+    auto softmax = [&]() {
+      float p[NT][4], wt[NT][4], top = 0.0f;
+      u32x2 vs[NT];
+      if constexpr (BITS < 16) {
+        // (a scale of zero, whose codes are zero, counts as fp16's smallest: p stays bounded)
+        const h2 least = __builtin_bit_cast(h2, 0x00010001u);
+#pragma unroll
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+          for (int k = 0; k < 2; k++) {
+            const uint32_t two = k == 0 ? vsr[i].x : vsr[i].y;
+            vs[i][k] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2, two), least));
+          }
+      }
+      auto weights = [&]() {
+#pragma unroll
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            p[i][j] = __builtin_amdgcn_exp2f(fmaf(s[i][j], c1, -m));
+            wt[i][j] = BITS < 16 ? fmaf(p[i][j], scale_of(vs[i], j), 0.0f) : p[i][j];
+            top = fmaxf(top, wt[i][j]);
+          }
+      };
+      weights();
+      if (__any(top > 256.0f)) {          // (also the first step: m is -infinity, top infinite)
+        float y = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NT; i++)
+#pragma unroll
+          for (int j = 0; j < 4; j++)
+            y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? __builtin_amdgcn_logf(scale_of(vs[i], j)) : 0.0f));
+        y = fmaxf(y, __shfl_xor(y, 16));
+        y = fmaxf(y, __shfl_xor(y, 32));
+        const float m1 = fmaxf(m, y);
         const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m1);
         m = m1;
         l *= f;
 #pragma unroll
         for (int i = 0; i < DV; i++) o[i] *= f;
+        weights();
       }
-      const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
       for (int i = 0; i < NT; i++)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-          s[i][j] = __builtin_amdgcn_exp2f(s[i][j] - ref);
-          l += s[i][j];
-          if constexpr (BITS < 16) s[i][j] *= vs[i][j];
+          l += p[i][j];
+          s[i][j] = wt[i][j];
         }
-      // O^T += V^T P^T, 32 tokens (two tiles) at a time
+    };
+    // O^T += V^T P^T, 32 tokens (two tiles) at a time
+    auto products = [&]() {
 #pragma unroll
       for (int i = 0; i < NT; i += 2) {
         u32x4 ph, pl;
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-          const float p0 = s[i + j / 2][2 * (j & 1)], p1 = s[i + j / 2][2 * (j & 1) + 1];
-          ph[j] = pack2<VBF>(p0, p1);
-          if constexpr (SPLIT)
-            pl[j] = pack2<true>(p0 - __builtin_bit_cast(float, ph[j] << 16),
-                                p1 - __builtin_bit_cast(float, ph[j] & 0xffff0000u));
+          const int h = i + j / 2, k = 2 * (j & 1);
+          ph[j] = pack2<VBF>(s[h][k], s[h][k + 1]);
+          const f2 u = unpack2<VBF>(ph[j]);
+          pl[j] = pack2<VBF>(s[h][k] - u.x, s[h][k + 1] - u.y);
         }
         // rows as 16-bit values, two channels a word: row[tile][j][channel / 2]
         uint32_t row[2][4][DV / 2];
@@ -348,19 +485,19 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a)
               for (int k = 0; k < DV / 2; k++) row[h][j][k] = raw[k];
             } else if constexpr (BITS == 8) {
 #pragma unroll
-              for (int k = 0; k < DV / 4; k++) widen4<true>(raw[k], 1.0f, row[h][j][2 * k], row[h][j][2 * k + 1]);
+              for (int k = 0; k < DV / 4; k++) widen4<VBF>(raw[k], 1.0f, row[h][j][2 * k], row[h][j][2 * k + 1]);
             } else if constexpr (VBr < 4) {
               // codes 0..3 of the shared word for even lanes, 4..7 for odd ones
               uint32_t lo, hi;
               tq4_to_fp8(raw[0], lo, hi);
-              widen4<true>(r & 1 ? hi : lo, 512.0f, row[h][j][0], row[h][j][1]);
+              widen4<VBF>(r & 1 ? hi : lo, 512.0f, row[h][j][0], row[h][j][1]);
             } else {
 #pragma unroll
               for (int k = 0; k < DV / 8; k++) {
                 uint32_t lo, hi;
                 tq4_to_fp8(raw[k], lo, hi);
-                widen4<true>(lo, 512.0f, row[h][j][4 * k], row[h][j][4 * k + 1]);
-                widen4<true>(hi, 512.0f, row[h][j][4 * k + 2], row[h][j][4 * k + 3]);
+                widen4<VBF>(lo, 512.0f, row[h][j][4 * k], row[h][j][4 * k + 1]);
+                widen4<VBF>(hi, 512.0f, row[h][j][4 * k + 2], row[h][j][4 * k + 3]);
               }
             }
           }
@@ -372,50 +509,92 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a)
           for (int j = 0; j < 4; j++)
             op[j] = __builtin_amdgcn_perm(row[j / 2][2 * (j & 1) + 1][c / 2], row[j / 2][2 * (j & 1)][c / 2], sel);
           o[c] = mfma16<VBF>(op, ph, o[c]);
-          if constexpr (SPLIT) o[c] = mfma16<VBF>(op, pl, o[c]);
+          o[c] = mfma16<VBF>(op, pl, o[c]);
         }
       }
+    };
+
+    // The keys of the next step are loaded as soon as this one's scores are formed, its
+    // values after the products, so that either is in flight while the other is computed
+    // on; page numbers a step earlier still.
+    if (steps > 0) {
+      int ahead[NT];
+#pragma unroll
+      for (int i = 0; i < NT; i++) ahead[i] = page_of(t0 + W * ST + 16 * i);
+      for (int u = 0; u < steps - 1; u++) {
+#pragma unroll
+        for (int i = 0; i < NT; i++) {
+          row[i] = row_of(ahead[i], t0 + W * ST + 16 * i);
+          ahead[i] = page_of(t0 + 2 * W * ST + 16 * i);
+        }
+        scores();
+        load_k(row);
+        if (t0 < rg.first) mask_scores();
+        softmax();
+        if (t0 < rg.first) mask_values();
+        products();
+        load_v(row);
+        t0 += W * ST;
+        const int done = x - x0 + W * u;
+        if (done >= quarter) {
+          if (done < 2 * quarter) __builtin_amdgcn_s_setprio(2);
+          else if (done < 3 * quarter) __builtin_amdgcn_s_setprio(1);
+          else __builtin_amdgcn_s_setprio(0);
+        }
+      }
+      const bool edge = t0 < rg.first || t0 + ST > rg.len;
+      scores();
+      if (edge) mask_scores();
+      softmax();
+      if (edge) mask_values();
+      products();
     }
 
     // the wavefronts' parts, joined: lane (r, g) holds channels DV (4 g + i) + c of head r
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (g == 0) {
-      lds_m[w][r] = m;
-      lds_l[w][r] = l;
+      lds_m[w * kHeads + r] = m;
+      lds_l[w * kHeads + r] = l;
     }
     if (r < heads) {
 #pragma unroll
       for (int i = 0; i < 4; i++)
 #pragma unroll
         for (int c = 0; c < DV; c += 4)
-          *reinterpret_cast<v4f *>(&lds_o[w][r][DV * (4 * g + i) + c]) = v4f{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+          *reinterpret_cast<v4f *>(&lds_o[(w * cols + r) * LD + DV * (4 * g + i) + c]) =
+              v4f{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     }
     __syncthreads();
-    const bool whole = n == rg.units;
-    float *slot = part + (x == x0 ? 0 : partial_floats(D, cols));
-    for (int e = threadIdx.x; e < heads * (D / 2); e += 64 * kWaves) {
-      const int h = e / (D / 2), d0 = 2 * (e % (D / 2));
-      float mm = lds_m[0][h];
+    const bool whole = n == rg.steps;
+    const int64_t row0 = (int64_t)b * a.hq + kvh * a.group + hb * kHeads;
+    const int slot = 2 * blockIdx.x + (x == x0 ? 0 : 1);
+    float *part = parts + (int64_t)slot * part_floats(D, cols);
+    if (!DIRECT && t == 0 && threadIdx.x == 0) {
+      const int end = x + rg.steps - 1;      // the range's last step
+      joins[(int64_t)b * vheads + vh] = Join{slot, whole ? 0 : end / chunk - (int)blockIdx.x + 1};
+    }
+    for (int e = threadIdx.x; e < heads * (D / 4); e += 64 * W) {
+      const int h = e / (D / 4), d0 = 4 * (e % (D / 4));
+      float mm = lds_m[h];
 #pragma unroll
-      for (int i = 1; i < kWaves; i++) mm = fmaxf(mm, lds_m[i][h]);
+      for (int i = 1; i < W; i++) mm = fmaxf(mm, lds_m[i * kHeads + h]);
       const float ref = mm == -INFINITY ? 0.0f : mm;
-      float ll = 0.0f, y0 = 0.0f, y1 = 0.0f;
+      float ll = 0.0f;
+      v4f y = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < kWaves; i++) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[i][h] - ref);
-        ll = fmaf(f, lds_l[i][h], ll);
-        y0 = fmaf(f, lds_o[i][h][d0], y0);
-        y1 = fmaf(f, lds_o[i][h][d0 + 1], y1);
+      for (int i = 0; i < W; i++) {
+        const float f = __builtin_amdgcn_exp2f(lds_m[i * kHeads + h] - ref);
+        const v4f z = *reinterpret_cast<const v4f *>(&lds_o[(i * cols + h) * LD + d0]);
+        ll = fmaf(f, lds_l[i * kHeads + h], ll);
+#pragma unroll
+        for (int k = 0; k < 4; k++) y[k] = fmaf(f, z[k], y[k]);
       }
-      const int qh = kvh * a.group + hb * kHeads + h;
       if (whole) {
-        const float inv = 1.0f / ll;
-        *reinterpret_cast<uint32_t *>(a.out + ((int64_t)b * a.hq + qh) * D + d0) = pack2<BF16>(y0 * inv, y1 * inv);
-        if (a.lse != nullptr && d0 == 0) a.lse[(int64_t)b * a.hq + qh] = (mm + log2f(ll)) * (1.0f / kLog2e);
+        store4<BF16>(a, D, row0 + h, d0, mm, ll, y);
       } else {
-        *reinterpret_cast<f2 *>(slot + partial_head(cols) + h * D + d0) = f2{y0, y1};
-        if (d0 == 0) *reinterpret_cast<f2 *>(slot + 2 * h) = f2{mm, ll};
+        *reinterpret_cast<v4f *>(part + part_head(cols) + h * D + d0) = y;
+        if (d0 == 0) *reinterpret_cast<f2 *>(part + 2 * h) = f2{mm, ll};
       }
     }
     x += n;
@@ -426,112 +605,119 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(const AttendArgs a)
         vh = 0;
         do {
           b++;
-          rg = range_of<UT>(uniform(a.lengths[b]), cap, a.window);
-        } while (rg.units == 0);
+          rg = range_of<ST>(uniform(a.lengths[b]), cap, a.window);
+        } while (rg.steps == 0);
       }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// Joins the parts of ranges that several work-groups hold, in their order, and
-// fills the rows of streams that hold nothing.  One work-group per stream and
-// query head.
+// The join, for ranges of more than one part: gridDim.z work-groups per range share
+// its heads, a work-group's threads its parts; every sum in an order of its own.
 // ---------------------------------------------------------------------------
-template <int D, int BITS, bool BF16>
-__global__ __launch_bounds__(256) void join_kernel(const AttendArgs a) {
-  constexpr int UT = unit_tokens(BITS);
-  constexpr int LN = D / 4, PG = 256 / LN;     // lanes per part, parts at a time
-  __shared__ float lds_o[PG][D];
-  __shared__ float lds_m[PG], lds_l[PG];
-  const int b = blockIdx.y, qh = blockIdx.x;
-  const int cap = a.max_pages << a.c.lps;
-  const int hblocks = (a.group + kHeads - 1) / kHeads, vheads = a.c.heads * hblocks;
-  const int cols = min(a.group, kHeads);
-  const Range rg = range_of<UT>(uniform(a.lengths[b]), cap, a.window);
-  uint16_t *out = a.out + ((int64_t)b * a.hq + qh) * D;
-  if (rg.units == 0) {
-    if (threadIdx.x < D / 2) reinterpret_cast<uint32_t *>(out)[threadIdx.x] = 0;
-    if (a.lse != nullptr && threadIdx.x == 0) a.lse[(int64_t)b * a.hq + qh] = -INFINITY;
-    return;
-  }
-  const int64_t total = (int64_t)units_before<UT>(a, cap, a.batch) * vheads;
-  const int64_t chunk = (total + a.blocks - 1) / a.blocks;
-  const int kvh = qh / a.group, hb = qh % a.group / kHeads, h = qh % a.group % kHeads;
-  const int64_t p0 = (int64_t)units_before<UT>(a, cap, b) * vheads + (int64_t)(kvh * hblocks + hb) * rg.units;
-  const int64_t w0 = p0 / chunk, w1 = (p0 + rg.units - 1) / chunk;
-  if (w0 == w1) return;                        // written by its work-group
-  const int pg = threadIdx.x / LN, d0 = 4 * (threadIdx.x % LN);
-  float m = -INFINITY, l = 0.0f;
-  v4f o = {0, 0, 0, 0};
-  for (int64_t w = w0 + pg; w <= w1; w += PG) {
-    const float *slot = a.scratch + (2 * w + (w * chunk >= p0 ? 0 : 1)) * partial_floats(D, cols);
-    const f2 ml = *reinterpret_cast<const f2 *>(slot + 2 * h);
-    const v4f y = *reinterpret_cast<const v4f *>(slot + partial_head(cols) + h * D + d0);
-    const float m1 = fmaxf(m, ml.x), ref = m1 == -INFINITY ? 0.0f : m1;
-    const float f0 = __builtin_amdgcn_exp2f(m - ref), f1 = __builtin_amdgcn_exp2f(ml.x - ref);
-    m = m1;
-    l = l * f0 + ml.y * f1;
+template <int D, bool BF16>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendArgs a) {
+  constexpr int Q = D / 4, GROUPS = kJoinThreads / Q;
+  __shared__ __attribute__((aligned(16))) float lds_o[GROUPS][D], lds_ml[GROUPS][2];
+  const int b = blockIdx.y, vh = blockIdx.x, vheads = gridDim.x;
+  const int hblocks = (a.group + kHeads - 1) / kHeads, cols = min(a.group, kHeads);
+  const Join *joins = reinterpret_cast<const Join *>(a.scratch + (int64_t)a.blocks * 2 * part_floats(D, cols));
+  const Join j = joins[(int64_t)b * vheads + vh];
+  if (j.parts == 0) return;                      // written by its work-group
+  const int kvh = vh / hblocks, hb = vh % hblocks;
+  const int heads = min(kHeads, a.group - hb * kHeads);
+  const int pg = threadIdx.x / Q, d0 = 4 * (threadIdx.x % Q);
+  for (int h = blockIdx.z; h < heads; h += gridDim.z) {
+    float m = -INFINITY, l = 0.0f;
+    v4f o = {0, 0, 0, 0};
+    auto add = [&](f2 ml, v4f y) {
+      const float m1 = fmaxf(m, ml.x), ref = m1 == -INFINITY ? 0.0f : m1;
+      const float f0 = __builtin_amdgcn_exp2f(m - ref), f1 = __builtin_amdgcn_exp2f(ml.x - ref);
+      m = m1;
+      l = l * f0 + ml.y * f1;
 #pragma unroll
-    for (int i = 0; i < 4; i++) o[i] = o[i] * f0 + y[i] * f1;
-  }
-  *reinterpret_cast<v4f *>(&lds_o[pg][d0]) = o;
-  if (d0 == 0) {
-    lds_m[pg] = m;
-    lds_l[pg] = l;
-  }
-  __syncthreads();
-  if (threadIdx.x >= D / 2) return;
-  const int e = 2 * threadIdx.x;
-  float mm = lds_m[0];
+      for (int i = 0; i < 4; i++) o[i] = o[i] * f0 + y[i] * f1;
+    };
+#pragma unroll 4
+    for (int k = pg; k < j.parts; k += GROUPS) {
+      const int slot = k == 0 ? j.first : (j.first & ~1) + 2 * k;
+      const float *part = a.scratch + (int64_t)slot * part_floats(D, cols);
+      add(*reinterpret_cast<const f2 *>(part + 2 * h), *reinterpret_cast<const v4f *>(part + part_head(cols) + h * D + d0));
+    }
+    if (pg > 0) {
+      *reinterpret_cast<v4f *>(&lds_o[pg][d0]) = o;
+      if (d0 == 0) *reinterpret_cast<f2 *>(lds_ml[pg]) = f2{m, l};
+    }
+    __syncthreads();
+    if (pg == 0) {
 #pragma unroll
-  for (int i = 1; i < PG; i++) mm = fmaxf(mm, lds_m[i]);
-  const float ref = mm == -INFINITY ? 0.0f : mm;
-  float ll = 0.0f, y0 = 0.0f, y1 = 0.0f;
-#pragma unroll
-  for (int i = 0; i < PG; i++) {
-    const float f = __builtin_amdgcn_exp2f(lds_m[i] - ref);
-    ll = fmaf(f, lds_l[i], ll);
-    y0 = fmaf(f, lds_o[i][e], y0);
-    y1 = fmaf(f, lds_o[i][e + 1], y1);
+      for (int k = 1; k < GROUPS; k++) add(*reinterpret_cast<const f2 *>(lds_ml[k]), *reinterpret_cast<const v4f *>(&lds_o[k][d0]));
+      store4<BF16>(a, D, (int64_t)b * a.hq + kvh * a.group + hb * kHeads + h, d0, m, l, o);
+    }
+    __syncthreads();
   }
-  const float inv = 1.0f / ll;
-  *reinterpret_cast<uint32_t *>(out + e) = pack2<BF16>(y0 * inv, y1 * inv);
-  if (a.lse != nullptr && e == 0) a.lse[(int64_t)b * a.hq + qh] = (mm + log2f(ll)) * (1.0f / kLog2e);
 }
 
+template <int W, int D, int BITS, bool BF16>
+hipError_t go_attend(const AttendArgs &a, hipStream_t s) {
+  const int cols = a.group < kHeads ? a.group : kHeads;
+  const int bytes = lds_floats(W, D, BITS, cols) * 4;
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(attend_kernel<W, D, BITS, BF16>), bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attend_kernel<W, D, BITS, BF16>), dim3(a.blocks), dim3(64 * W), bytes, s, a);
+  return hipGetLastError();
+}
 template <int D, int BITS, bool BF16>
-void go(const AttendArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((attend_kernel<D, BITS, BF16>), dim3(a.blocks), dim3(64 * kWaves), 0, s, a);
-  hipLaunchKernelGGL((join_kernel<D, BITS, BF16>), dim3(a.hq, a.batch), dim3(256), 0, s, a);
+hipError_t go(const AttendArgs &a, hipStream_t s) {
+  if (a.direct) return go_attend<kDirectWaves, D, BITS, BF16>(a, s);
+  const hipError_t e = go_attend<kRunWaves, D, BITS, BF16>(a, s);
+  if (e != hipSuccess) return e;
+  // (about 512 work-groups, or one for every range)
+  const int vheads = a.c.heads * ((a.group + kHeads - 1) / kHeads), cols = a.group < kHeads ? a.group : kHeads;
+  const int share = 512 / (vheads * a.batch);
+  hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(vheads, a.batch, share < 1 ? 1 : share < cols ? share : cols),
+                     dim3(kJoinThreads), 0, s, a);
+  return hipGetLastError();
 }
 template <int D>
-void go_bits(const AttendArgs &a, bool bf16, hipStream_t s) {
-  if (a.c.bits == 16) bf16 ? go<D, 16, true>(a, s) : go<D, 16, false>(a, s);
-  else if (a.c.bits == 8) bf16 ? go<D, 8, true>(a, s) : go<D, 8, false>(a, s);
-  else bf16 ? go<D, 4, true>(a, s) : go<D, 4, false>(a, s);
+hipError_t go_bits(const AttendArgs &a, bool bf16, hipStream_t s) {
+  if (a.c.bits == 16) return bf16 ? go<D, 16, true>(a, s) : go<D, 16, false>(a, s);
+  if (a.c.bits == 8) return bf16 ? go<D, 8, true>(a, s) : go<D, 8, false>(a, s);
+  return bf16 ? go<D, 4, true>(a, s) : go<D, 4, false>(a, s);
 }
 
 }  // namespace
 
-int attend_blocks(const KvCache &c, int batch, int hq, int64_t max_len) {
-  const int group = hq / c.heads, ut = unit_tokens(c.bits);
-  // (one unit more: a window may start within a tile)
-  const int64_t units = (max_len + 15 + ut - 1) / ut * batch * c.heads * ((group + kHeads - 1) / kHeads);
-  const int64_t most = 256 * 3;
-  return (int)(units < most ? units : most);
-}
-
-size_t attend_scratch_bytes(const KvCache &c, int batch, int hq, int64_t max_len) {
-  const int group = hq / c.heads;
-  return (size_t)attend_blocks(c, batch, hq, max_len) * 2 * partial_floats(c.d, group < kHeads ? group : kHeads) * 4;
+AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window) {
+  AttendPlan p;
+  const int group = hq / c.heads, st = step_tokens(c.d, c.bits);
+  const int64_t ranges = (int64_t)batch * c.heads * ((group + kHeads - 1) / kHeads);
+  // (15 tokens more: a window may start within a tile)
+  const int64_t longest = window > 0 && window < max_len ? window + 15 : max_len;
+  const int64_t steps = (longest + st - 1) / st;
+  // One work-group per range where that takes two rounds of its wavefronts, or four
+  // if the ranges alone fill the CUs (8 kv heads of 128; graph replays, us, direct
+  // against runs and their join: 1 stream of 512 tokens 8.0 against 8.0, of 1024
+  // 12.1 against 8.4; 32 streams of 1024 22.4 against 29.8; one stream of 1024
+  // among short ones costs 4 more).
+  p.direct = steps <= (ranges >= 256 ? 32 : 16) && ranges < ((int64_t)1 << 31);
+  p.steps = ranges * steps;
+  if (p.direct) {
+    p.blocks = (int)ranges;
+    p.scratch = 0;
+    return p;
+  }
+  const int64_t runs = (p.steps + kRunWaves - 1) / kRunWaves;
+  p.blocks = (int)(runs < kMostRuns ? runs : kMostRuns);
+  p.scratch = (size_t)p.blocks * 2 * part_floats(c.d, group < kHeads ? group : kHeads) * 4 + (size_t)ranges * sizeof(Join);
+  return p;
 }
 
 hipError_t launch_attend(const AttendArgs &a, bool bf16, hipStream_t s) {
-  if (a.c.d == 64) go_bits<64>(a, bf16, s);
-  else if (a.c.d == 128) go_bits<128>(a, bf16, s);
-  else go_bits<256>(a, bf16, s);
-  return hipGetLastError();
+  if (a.c.d == 64) return go_bits<64>(a, bf16, s);
+  if (a.c.d == 128) return go_bits<128>(a, bf16, s);
+  return go_bits<256>(a, bf16, s);
 }
 
 }  // namespace tq

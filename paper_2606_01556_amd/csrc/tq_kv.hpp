@@ -64,14 +64,21 @@ struct AttendArgs {
   uint16_t *out;             // [batch][hq][d]
   float *lse;                // [batch][hq] or null
   float *scratch;
-  int blocks;                // work-groups of the first launch
+  int blocks;                // work-groups
+  int direct;
 };
 
 hipError_t launch_tokens(const TokenArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_kv_read(const ReadArgs &a, bool bf16, hipStream_t s);
-// work-groups of the attention for at most max_len tokens in each of batch streams
-int attend_blocks(const KvCache &c, int batch, int hq, int64_t max_len);
-size_t attend_scratch_bytes(const KvCache &c, int batch, int hq, int64_t max_len);
+// How an attention call is cut, by what the host knows of it: direct, one
+// work-group per (stream, head) range and no scratch, or runs of all ranges.
+struct AttendPlan {
+  bool direct;
+  int blocks;
+  int64_t steps;           // upper bound of all ranges' steps
+  size_t scratch;          // bytes
+};
+AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window);
 hipError_t launch_attend(const AttendArgs &a, bool bf16, hipStream_t s);
 
 // row / d for 0 <= row < 2^31 and 2 <= d < 2^31: with L = ceil(log2 d) and

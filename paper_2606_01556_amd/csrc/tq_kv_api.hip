@@ -162,19 +162,21 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
   return hip_status(tq::launch_kv_read(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
-static tq_status attention_shape(const tq_kv_cache *c, int batch, int q_heads, int max_pages) {
+static tq_status attention_plan(const tq_kv_cache *c, const tq::KvCache &k, int batch, int q_heads, int max_pages,
+                                int window, tq::AttendPlan &p) {
   if (batch < 0 || batch > 65535 || q_heads < 1 || q_heads > 65535 || q_heads % c->kv_heads != 0 || max_pages < 1 ||
-      (int64_t)max_pages * c->page_size > ((int64_t)1 << 30) ||
-      // (the kernels sum the streams' units, of 128 tokens or more, in 31 bits)
-      (int64_t)batch * (((int64_t)max_pages * c->page_size + 142) / 128) >= ((int64_t)1 << 31))
+      (int64_t)max_pages * c->page_size > ((int64_t)1 << 30) || window < 0)
     return TQ_ERR_SHAPE;
-  return TQ_OK;
+  p = tq::attend_plan(k, batch, q_heads, (int64_t)max_pages * c->page_size, window);
+  // (the kernel numbers the steps of all streams and heads in 31 bits)
+  return p.steps < ((int64_t)1 << 31) - ((int64_t)1 << 16) ? TQ_OK : TQ_ERR_SHAPE;
 }
 
-size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int max_pages) {
+size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int max_pages, int window) {
   tq::KvCache k;
-  if (check_cache(c, k) != TQ_OK || attention_shape(c, batch, q_heads, max_pages) != TQ_OK) return 0;
-  return tq::attend_scratch_bytes(k, batch, q_heads, (int64_t)max_pages * c->page_size);
+  tq::AttendPlan p;
+  if (check_cache(c, k) != TQ_OK || attention_plan(c, k, batch, q_heads, max_pages, window, p) != TQ_OK) return 0;
+  return p.scratch;
 }
 
 tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
@@ -186,14 +188,14 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
   TQ_TRY(check_cache(c, a.c));
   tq::HeadRows rows;
   TQ_TRY(check_rows(q, rows));
-  TQ_TRY(attention_shape(c, batch, q_heads, max_pages));
-  if (window < 0 || table_stride < 0 || !std::isfinite(scale)) return TQ_ERR_SHAPE;
+  tq::AttendPlan p;
+  TQ_TRY(attention_plan(c, a.c, batch, q_heads, max_pages, window, p));
+  if (table_stride < 0 || !std::isfinite(scale)) return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
   if (!aligned(page_table, 4) || !aligned(lengths, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(scratch))
     return TQ_ERR_ALIGN;
   if (batch == 0) return TQ_OK;
-  if (scratch == nullptr) return TQ_ERR_NULL;
-  const int64_t max_len = (int64_t)max_pages * c->page_size;
+  if (p.scratch != 0 && scratch == nullptr) return TQ_ERR_NULL;
   a.q = rows.p; a.q_ts = rows.ts; a.q_hs = rows.hs;
   a.batch = batch; a.hq = q_heads; a.group = q_heads / c->kv_heads;
   a.table = page_table; a.table_stride = table_stride; a.max_pages = max_pages;
@@ -202,7 +204,8 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
   a.out = static_cast<uint16_t *>(out);
   a.lse = lse;
   a.scratch = static_cast<float *>(scratch);
-  a.blocks = tq::attend_blocks(a.c, batch, q_heads, max_len);
+  a.direct = p.direct;
+  a.blocks = p.blocks;
   return hip_status(tq::launch_attend(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 

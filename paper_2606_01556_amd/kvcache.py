@@ -52,7 +52,7 @@ def declare(L):
     L.tq_kv_append.argtypes = [C, H, H, P, I, I, P]
     L.tq_qk_norm_rope_append.argtypes = [N, C, H, H, H, P, I, I, I, P, P, P]
     L.tq_kv_read.argtypes = [C, P, I, P, P, I, P]
-    L.tq_paged_attention_scratch_bytes.argtypes = [C, I, I, I]
+    L.tq_paged_attention_scratch_bytes.argtypes = [C, I, I, I, I]
     L.tq_paged_attention_scratch_bytes.restype = ctypes.c_size_t
     L.tq_paged_attention.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, ctypes.c_float, I, P, P, P, P]
 
@@ -383,14 +383,17 @@ def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None 
         scale = 1.0 / math.sqrt(d)
     st = _stream(stream)
     L = lib()
-    nscratch = L.tq_paged_attention_scratch_bytes(c, batch, hq, pages)
-    specs = [((batch, hq, d), dtype), ((nscratch // 4,), torch.float32)]
+    nscratch = L.tq_paged_attention_scratch_bytes(c, batch, hq, pages, window)
+    specs = [((batch, hq, d), dtype)]
     if return_lse:
         specs.append(((batch, hq), torch.float32))
+    if nscratch:
+        specs.append(((nscratch // 4,), torch.float32))
     out = _new(stream, st, dev, (q, page_table, lengths), *specs)
     if batch:
         _check(L.tq_paged_attention(c, qr, TQ_BF16 if dtype is _types()[1] else TQ_F16, batch, hq,
                                     page_table.data_ptr(), stride, pages, lp, scale, window,
-                                    out[0].data_ptr(), out[2].data_ptr() if return_lse else None,
-                                    out[1].data_ptr(), st), "tq_paged_attention")
-    return (out[0], out[2]) if return_lse else out[0]
+                                    out[0].data_ptr(), out[1].data_ptr() if return_lse else None,
+                                    out[-1].data_ptr() if nscratch else None, st),
+               "tq_paged_attention")
+    return (out[0], out[1]) if return_lse else out[0]

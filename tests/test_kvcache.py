@@ -140,7 +140,7 @@ def test_cache_validation(over, code):
     assert L.tq_kv_read(c, FAKE, 0, FAKE, FAKE, 0, None) == code
     assert L.tq_qk_norm_rope_append(rope(), c, ROWS, ROWS, ROWS, FAKE, 0, 2, 0, FAKE, None, None) == code
     assert L.tq_paged_attention(c, ROWS, 0, 0, 2, FAKE, 4, 4, FAKE, 1.0, 0, FAKE, None, FAKE, None) == code
-    assert L.tq_paged_attention_scratch_bytes(c, 1, 2, 4) == 0
+    assert L.tq_paged_attention_scratch_bytes(c, 1, 2, 400, 0) == 0
 
 
 def test_append_and_read_validation():
@@ -190,16 +190,19 @@ def test_attention_validation():
         return L.tq_paged_attention(c or desc(), q, dt, b, hq, pt, stride, pages, ln, scale, window, out, lse, scratch, None)
 
     assert call() == 0 and call(scratch=None) == 0
-    assert call(b=1, scratch=None) == 1 and call(q=None) == 1 and call(pt=None) == 1 and call(ln=None) == 1
+    assert call(b=1, pages=400, scratch=None) == 1 and call(q=None) == 1 and call(pt=None) == 1 and call(ln=None) == 1
     assert call(out=None) == 1
     for bad in (dict(b=-1), dict(b=65536), dict(hq=0), dict(hq=3), dict(hq=65536), dict(pages=0), dict(pages=(1 << 26) + 1),
                 dict(window=-1), dict(stride=-4), dict(scale=math.nan), dict(scale=math.inf)):
         assert call(**bad) == 2, bad
     assert call(dt=1) == 5 and call(dt=3, c=desc(bits=4, k_scales=FAKE, v_scales=FAKE)) == 5
     assert call(out=FAKE + 8) == 6 and call(lse=FAKE + 2) == 6 and call(scratch=FAKE + 8) == 6 and call(pt=FAKE + 2) == 6
-    assert L.tq_paged_attention_scratch_bytes(desc(), 1, 3, 4) == 0
-    assert L.tq_paged_attention_scratch_bytes(None, 1, 4, 4) == 0
-    assert 0 < L.tq_paged_attention_scratch_bytes(desc(), 1, 4, 4) < L.tq_paged_attention_scratch_bytes(desc(), 9, 4, 400)
+    assert call(b=65535, pages=1 << 20) == 2
+    size = lambda *a: L.tq_paged_attention_scratch_bytes(*a)
+    assert size(desc(), 1, 3, 400, 0) == 0 and size(None, 1, 4, 400, 0) == 0 and size(desc(), 1, 4, 400, -1) == 0
+    assert 0 < size(desc(), 1, 4, 400, 0) < size(desc(), 9, 4, 400, 0)
+    # short streams: a work-group holds a range whole
+    assert size(desc(), 9, 4, 4, 0) == 0 and size(desc(), 9, 4, 400, 100) == 0
 
 
 def test_binding_refuses_host_tensors():
