@@ -17,9 +17,9 @@ A decode step of one block:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
-import math
 
 from . import TQ_BF16, TQ_F16, _check, _other_stream, _stream, lib
 
@@ -58,35 +58,38 @@ def declare(L):
 
 
 # ------------------------------------------------------------------ argument checks
-def _gpu(t, name, dtype, device=None):
+# The usual tensor passes a chain of tests (about 0.3 us); where one fails, a second
+# look says which.  get_device() is -1 for a host tensor.
+def _refuse(t, name, dtypes, device):
     import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a GPU tensor")
-    if t.dtype not in dtype:
-        raise TypeError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtype))}")
-    if device is not None and t.get_device() != device:
-        raise ValueError(f"{name}: on device {t.get_device()}, the cache or q is on {device}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on device {t.get_device()}, the others are on {device}")
 
 
 def _plain(t, name, dtype, shape, device):
     """The address of a contiguous tensor of one type and shape."""
-    import torch
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous() or t.get_device() != device:
-        _gpu(t, name, (dtype,), device)
+    if not (isinstance(t, _torch().Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == device
+            and t.is_contiguous()):
+        _refuse(t, name, (dtype,), device)
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
         raise ValueError(f"{name}: must be contiguous")
     return t.data_ptr()
 
 
-def _rows(t, name, dtype, device, heads=None, head_dim=None, tokens=None):
-    """The tq_head_rows of t [tokens, heads, head_dim]."""
-    _gpu(t, name, dtype, device)
+def _rows(t, name, dtypes, device, tokens, heads, head_dim):
+    """The tq_head_rows of t [tokens, heads, head_dim] (None: any number)."""
+    if not (isinstance(t, _torch().Tensor) and t.dtype in dtypes and t.get_device() == device):
+        _refuse(t, name, dtypes, device)
     shape = t.shape
-    if len(shape) != 3 or (heads is not None and shape[1] != heads) or (
-            head_dim is not None and shape[2] != head_dim) or (tokens is not None and shape[0] != tokens):
+    if len(shape) != 3 or not (tokens is None or shape[0] == tokens) or not (
+            heads is None or shape[1] == heads) or shape[2] != head_dim:
         want = ", ".join(n if v is None else str(v) for n, v in (("tokens", tokens), ("heads", heads),
                                                                  ("head_dim", head_dim)))
         raise ValueError(f"{name}: shape {tuple(shape)}, expected [{want}]")
@@ -96,46 +99,61 @@ def _rows(t, name, dtype, device, heads=None, head_dim=None, tokens=None):
     if shape[1] <= 1:
         hs = 0
     p = t.data_ptr()
-    if ds != 1 or ts % 8 or hs % 8 or p % 16:
+    if ds != 1 or (ts | hs) & 7 or p & 15:
         raise ValueError(f"{name}: rows must be contiguous and start on 16 bytes (strides {tuple(t.stride())}, "
                          f"address {p:#x}); pass {name}.contiguous()")
     return _HeadRows(p, ts, hs)
 
 
-def _current_device():
-    import torch
-    return torch._C._cuda_getDevice()
-
-
 def _on_device(device, name):
-    if device != _current_device():
-        raise ValueError(f"{name}: on device {device}, but the current device is {_current_device()}")
+    here = _torch()._C._cuda_getDevice()
+    if device != here:
+        raise ValueError(f"{name}: on device {device}, but the current device is {here}")
 
 
-def _new(stream, st, device, inputs, *specs):
-    """Tensors of the given (shape, dtype), and a scratch among them, from the memory
-    of the stream that the work runs on; on a stream other than the current one they
-    may be used and dropped on the current one, and the inputs stay until that stream
-    is done with them."""
+def _other(stream, st, device, inputs):
+    """`stream` as a torch stream where it is not the current one, else None; the
+    inputs then stay until that stream is done with them."""
+    torch = _torch()
+    other = _other_stream(stream, st, torch.device("cuda", device))
+    if other is not None:
+        for t in inputs:
+            if t is not None:
+                t.record_stream(other)
+    return other
+
+
+def _new(stream, st, device, inputs, like, *shapes):
+    """Tensors like `like` of the given shapes (a number: so many float32), from the
+    memory of the stream that the work runs on; on a stream other than the current
+    one they may be used and dropped on the current one."""
+    torch = _torch()
+    new = (like if type(like) is torch.Tensor else like.as_subclass(torch.Tensor)).new_empty
+    if stream is not None and (other := _other(stream, st, device, inputs)) is not None:
+        with torch.cuda.stream(other):
+            out = [new(s) if type(s) is tuple else new(s, dtype=torch.float32) for s in shapes]
+        here = torch.cuda.current_stream(device)
+        for t in out:
+            t.record_stream(here)
+        return out
+    return [new(s) if type(s) is tuple else new(s, dtype=torch.float32) for s in shapes]
+
+
+@functools.lru_cache(maxsize=None)
+def _torch():
     import torch
-    other = None if stream is None else _other_stream(stream, st, torch.device("cuda", device))
-    if other is None:
-        return [torch.empty(s, dtype=d, device=device) for s, d in specs]
-    with torch.cuda.stream(other):
-        out = [torch.empty(s, dtype=d, device=device) for s, d in specs]
-    here = torch.cuda.current_stream(device)
-    for t in out:
-        t.record_stream(here)
-    for t in inputs:
-        if t is not None:
-            t.record_stream(other)
-    return out
+    return torch
 
 
 @functools.lru_cache(maxsize=None)
 def _types():
     import torch
     return torch.float16, torch.bfloat16
+
+
+def _at(stream, device):
+    """The hipStream_t of `stream`, by default the current one."""
+    return _torch()._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
 
 
 # ------------------------------------------------------------------ the cache
@@ -152,12 +170,14 @@ class KVCache:
     least 16.  Slot number = page * page_size + place in the page.  The object holds
     the tensors and no state: which slots are in use is the program's to know."""
 
-    __slots__ = ("_t", "_c", "pages", "page_size", "kv_heads", "head_dim", "bits", "device")
+    __slots__ = ("_t", "_c", "_dtypes", "pages", "page_size", "kv_heads", "head_dim", "bits", "device")
 
     def __init__(self, k, v, k_scales=None, v_scales=None):
-        import torch
+        torch = _torch()
         f16, bf16 = _types()
-        _gpu(k, "k", (f16, bf16, torch.float8_e4m3fn, torch.int32))
+        kinds = (f16, bf16, torch.float8_e4m3fn, torch.int32)
+        if not (isinstance(k, torch.Tensor) and k.is_cuda and k.dtype in kinds):
+            _refuse(k, "k", kinds, None)
         if k.dim() != 4:
             raise ValueError(f"k: shape {tuple(k.shape)}, expected [pages, kv_heads, page_size, row]")
         shape, dev = k.shape, k.get_device()
@@ -183,15 +203,12 @@ class KVCache:
         self._c = _CacheDesc(pages, size, heads, d, bits, TQ_BF16 if k.dtype is bf16 else TQ_F16, kp, vp, ks, vs)
         self.pages, self.page_size, self.kv_heads, self.head_dim = pages, size, heads, d
         self.bits, self.device = bits, dev
+        self._dtypes = (k.dtype,) if bits == 16 else _types()    # of rows written, read or asked with
 
     k = property(lambda self: self._t[0])
     v = property(lambda self: self._t[1])
     k_scales = property(lambda self: self._t[2])
     v_scales = property(lambda self: self._t[3])
-
-    def _dtypes(self):
-        """Types that rows written or read may have."""
-        return (self._t[0].dtype,) if self.bits == 16 else _types()
 
 
 def empty_kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, bits: int = 16,
@@ -231,10 +248,10 @@ def _is_cache(cache):
 
 
 def _slots(slots, device, tokens=None):
-    import torch
+    torch = _torch()
     if not isinstance(slots, torch.Tensor) or slots.dim() != 1:
         raise ValueError("slots: expected an int64 tensor [tokens]")
-    return _plain(slots, "slots", torch.int64, (slots.shape[0] if tokens is None else tokens,), device)
+    return _plain(slots, "slots", torch.int64, slots.shape if tokens is None else (tokens,), device)
 
 
 def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
@@ -242,17 +259,17 @@ def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
     quantized where it has 8 or 4 bits (tq_kv_append).  A token whose slot is
     negative is not written; slots of one call are distinct."""
     c = _is_cache(cache)
-    types, dev = cache._dtypes(), cache.device
-    kr = _rows(k, "k", types, dev, cache.kv_heads, cache.head_dim)
-    tokens = k.shape[0]
-    vr = _rows(v, "v", (k.dtype,), dev, cache.kv_heads, cache.head_dim, tokens)
+    dev, heads, d = cache.device, cache.kv_heads, cache.head_dim
+    kr = _rows(k, "k", cache._dtypes, dev, None, heads, d)
+    tokens, dtype = k.shape[0], k.dtype
+    vr = _rows(v, "v", (dtype,), dev, tokens, heads, d)
     sp = _slots(slots, dev, tokens)
     if tokens == 0:
         return
-    st = _stream(stream)
+    st = _at(stream, dev)
     if stream is not None:
-        _new(stream, st, dev, (k, v, slots))
-    _check(lib().tq_kv_append(c, kr, vr, sp, tokens, TQ_BF16 if k.dtype is _types()[1] else TQ_F16, st),
+        _other(stream, st, dev, (k, v, slots))
+    _check(lib().tq_kv_append(c, kr, vr, sp, tokens, TQ_F16 if dtype is _types()[0] else TQ_BF16, st),
            "tq_kv_append")
 
 
@@ -270,25 +287,34 @@ def kv_read(cache: KVCache, slots, bf16: bool | None = None, stream=None):
             raise TypeError(f"bf16: the cache holds {dtype}")
     else:
         dtype = _types()[bool(bf16)]
-    st = _stream(stream)
-    shape = (tokens, cache.kv_heads, cache.head_dim)
-    ko, vo = _new(stream, st, dev, (slots,), (shape, dtype), (shape, dtype))
+    st = _at(stream, dev)
+    torch = _torch()
+    other = None if stream is None else _other(stream, st, dev, (slots,))
+    with torch.cuda.stream(other) if other is not None else _NO_STREAM:
+        k, v = torch.empty((2, tokens, cache.kv_heads, cache.head_dim), dtype=dtype, device=dev).unbind()
+    if other is not None:
+        k.record_stream(torch.cuda.current_stream(dev))      # (v is in the same memory)
     if tokens:
-        _check(lib().tq_kv_read(c, sp, tokens, ko.data_ptr(), vo.data_ptr(),
-                                TQ_BF16 if dtype is _types()[1] else TQ_F16, st), "tq_kv_read")
-    return ko, vo
+        _check(lib().tq_kv_read(c, sp, tokens, k.data_ptr(), v.data_ptr(),
+                                TQ_F16 if dtype is _types()[0] else TQ_BF16, st), "tq_kv_read")
+    return k, v
+
+
+_NO_STREAM = contextlib.nullcontext()
 
 
 def _norm_rope(positions, table, q_weight, k_weight, eps, interleaved, tokens, head_dim, dtype, dev):
-    import torch
-    qw = None if q_weight is None else _plain(q_weight, "q_weight", dtype, (head_dim,), dev)
-    kw = None if k_weight is None else _plain(k_weight, "k_weight", dtype, (head_dim,), dev)
+    torch = _torch()
+    shape = (head_dim,)
+    qw = None if q_weight is None else _plain(q_weight, "q_weight", dtype, shape, dev)
+    kw = None if k_weight is None else _plain(k_weight, "k_weight", dtype, shape, dev)
     if table is None:
         return _NormRope(qw, kw, None, None, 0, 0, 0, eps)
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table: expected a float32 tensor [max_positions, rotary_dim]")
-    n, rot = table.shape
-    tp = _plain(table, "table", torch.float32, (n, rot), dev)
+    shape = table.shape
+    tp = _plain(table, "table", torch.float32, shape, dev)
+    n, rot = shape
     if not 0 < rot <= head_dim or rot % 16 or n < 1:
         raise ValueError(f"table: {n} positions of {rot} values; a multiple of 16 up to head_dim {head_dim}")
     if positions is None:
@@ -305,21 +331,21 @@ def qk_norm_rope(q, k, positions, table, q_weight=None, k_weight=None, eps: floa
     None: no rotation), in fp32, rounded once (tq_qk_norm_rope).  q and k may be
     views of a fused projection's output."""
     types = _types()
-    _gpu(q, "q", types)
-    dev, dtype = q.get_device(), q.dtype
+    if not (isinstance(q, _torch().Tensor) and q.is_cuda and q.dtype in types):
+        _refuse(q, "q", types, None)
+    dev, dtype, shape = q.get_device(), q.dtype, q.shape
     _on_device(dev, "q")
-    qr = _rows(q, "q", types, dev)
-    tokens, hq, d = q.shape
-    if d not in (64, 128, 256):
-        raise ValueError(f"q: head_dim {d}; 64, 128 or 256 are supported")
-    kr = _rows(k, "k", (dtype,), dev, None, d, tokens)
+    if len(shape) != 3 or shape[2] not in (64, 128, 256):
+        raise ValueError(f"q: shape {tuple(shape)}; [tokens, heads, head_dim] with head_dim 64, 128 or 256")
+    tokens, hq, d = shape
+    qr = _rows(q, "q", types, dev, tokens, hq, d)
+    kr = _rows(k, "k", (dtype,), dev, tokens, None, d)
     hkv = k.shape[1]
     p = _norm_rope(positions, table, q_weight, k_weight, eps, interleaved, tokens, d, dtype, dev)
-    st = _stream(stream)
-    qo, ko = _new(stream, st, dev, (q, k, positions, table, q_weight, k_weight), ((tokens, hq, d), dtype),
-                  ((tokens, hkv, d), dtype))
+    st = _at(stream, dev)
+    qo, ko = _new(stream, st, dev, (q, k, positions, table, q_weight, k_weight), q, (tokens, hq, d), (tokens, hkv, d))
     if tokens:
-        _check(lib().tq_qk_norm_rope(p, qr, kr, tokens, hq, hkv, d, TQ_BF16 if dtype is types[1] else TQ_F16,
+        _check(lib().tq_qk_norm_rope(p, qr, kr, tokens, hq, hkv, d, TQ_F16 if dtype is types[0] else TQ_BF16,
                                      qo.data_ptr(), ko.data_ptr(), st), "tq_qk_norm_rope")
     return qo, ko
 
@@ -330,25 +356,26 @@ def qk_norm_rope_append(cache: KVCache, q, k, v, positions, table, slots, q_weig
     rotated q back, the rotated k and v into the cache at slots [tokens] int64.  With
     return_k (q, k), the k as it was before the cache's quantizer."""
     c = _is_cache(cache)
-    types, dev, d, hkv = cache._dtypes(), cache.device, cache.head_dim, cache.kv_heads
-    qr = _rows(q, "q", types, dev, None, d)
+    dev, d, hkv = cache.device, cache.head_dim, cache.kv_heads
+    qr = _rows(q, "q", cache._dtypes, dev, None, None, d)
     tokens, hq, _ = q.shape
     dtype = q.dtype
-    kr = _rows(k, "k", (dtype,), dev, hkv, d, tokens)
-    vr = _rows(v, "v", (dtype,), dev, hkv, d, tokens)
+    kr = _rows(k, "k", (dtype,), dev, tokens, hkv, d)
+    vr = _rows(v, "v", (dtype,), dev, tokens, hkv, d)
     sp = _slots(slots, dev, tokens)
     p = _norm_rope(positions, table, q_weight, k_weight, eps, interleaved, tokens, d, dtype, dev)
-    st = _stream(stream)
-    specs = [((tokens, hq, d), dtype)]
+    st = _at(stream, dev)
+    inputs = (q, k, v, positions, table, slots, q_weight, k_weight)
     if return_k:
-        specs.append(((tokens, hkv, d), dtype))
-    out = _new(stream, st, dev, (q, k, v, positions, table, slots, q_weight, k_weight), *specs)
+        qo, ko = _new(stream, st, dev, inputs, q, (tokens, hq, d), (tokens, hkv, d))
+    else:
+        (qo,), ko = _new(stream, st, dev, inputs, q, (tokens, hq, d)), None
     if tokens:
         _check(lib().tq_qk_norm_rope_append(p, c, qr, kr, vr, sp, tokens, hq,
-                                            TQ_BF16 if dtype is _types()[1] else TQ_F16, out[0].data_ptr(),
-                                            out[1].data_ptr() if return_k else None, st),
+                                            TQ_F16 if dtype is _types()[0] else TQ_BF16, qo.data_ptr(),
+                                            None if ko is None else ko.data_ptr(), st),
                "tq_qk_norm_rope_append")
-    return tuple(out) if return_k else out[0]
+    return (qo, ko) if return_k else qo
 
 
 def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None = None, window: int = 0,
@@ -359,41 +386,41 @@ def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None 
     them.  window > 0: only the last so many.  scale: head_dim^-1/2 by default.
     Returns out [batch, q_heads, head_dim] of q's type, zeros for a stream of length
     0; with return_lse (out, lse [batch, q_heads] float32)."""
-    import torch
     c = _is_cache(cache)
+    torch = _torch()
     dev, d = cache.device, cache.head_dim
-    qr = _rows(q, "q", cache._dtypes(), dev, None, d)
+    qr = _rows(q, "q", cache._dtypes, dev, None, None, d)
     batch, hq, _ = q.shape
-    dtype = q.dtype
     if hq == 0 or hq % cache.kv_heads:
         raise ValueError(f"q: {hq} heads are no multiple of the cache's {cache.kv_heads}")
-    _gpu(page_table, "page_table", (torch.int32,), dev)
-    if page_table.dim() != 2 or page_table.shape[0] != batch:
-        raise ValueError(f"page_table: shape {tuple(page_table.shape)}, expected [{batch}, max_pages]")
-    pages = page_table.shape[1]
+    if not (isinstance(page_table, torch.Tensor) and page_table.dtype is torch.int32 and page_table.get_device() == dev):
+        _refuse(page_table, "page_table", (torch.int32,), dev)
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] != batch or shape[1] == 0:
+        raise ValueError(f"page_table: shape {tuple(shape)}, expected [{batch}, max_pages]")
+    pages = shape[1]
     stride, step = page_table.stride()
     if (step != 1 and pages > 1) or (stride < pages and batch > 1):
         raise ValueError("page_table: rows must be contiguous")
     lp = _plain(lengths, "lengths", torch.int32, (batch,), dev)
     if window < 0:
         raise ValueError(f"window {window}: must not be negative")
-    if pages == 0:
-        raise ValueError("page_table: no pages")
     if scale is None:
-        scale = 1.0 / math.sqrt(d)
-    st = _stream(stream)
+        scale = d ** -0.5
+    st = _at(stream, dev)
     L = lib()
     nscratch = L.tq_paged_attention_scratch_bytes(c, batch, hq, pages, window)
-    specs = [((batch, hq, d), dtype)]
-    if return_lse:
-        specs.append(((batch, hq), torch.float32))
+    shapes = [(batch, hq, d)]
     if nscratch:
-        specs.append(((nscratch // 4,), torch.float32))
-    out = _new(stream, st, dev, (q, page_table, lengths), *specs)
+        shapes.append(nscratch // 4)
+    if return_lse:
+        shapes.append(batch * hq)
+    out = _new(stream, st, dev, (q, page_table, lengths), q, *shapes)
+    y = out[0]
+    lse = out[-1].view(batch, hq) if return_lse else None
     if batch:
-        _check(L.tq_paged_attention(c, qr, TQ_BF16 if dtype is _types()[1] else TQ_F16, batch, hq,
-                                    page_table.data_ptr(), stride, pages, lp, scale, window,
-                                    out[0].data_ptr(), out[1].data_ptr() if return_lse else None,
-                                    out[-1].data_ptr() if nscratch else None, st),
-               "tq_paged_attention")
-    return (out[0], out[1]) if return_lse else out[0]
+        _check(L.tq_paged_attention(c, qr, TQ_F16 if q.dtype is _types()[0] else TQ_BF16, batch, hq,
+                                    page_table.data_ptr(), stride, pages, lp, scale, window, y.data_ptr(),
+                                    None if lse is None else lse.data_ptr(),
+                                    out[1].data_ptr() if nscratch else None, st), "tq_paged_attention")
+    return (y, lse) if return_lse else y
