@@ -1,11 +1,15 @@
-"""Build libtq.so (the HIP kernels and the C ABI) in place for gfx950."""
+"""Build libtq.so (the HIP kernels and the C ABI) in place for gfx950, and _tqtorch.so
+(the native half of kvcache.py, against torch)."""
 import glob
 import os
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libtq.so")
+BINDING = os.path.join(HERE, "_tqtorch.so")
+CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -29,7 +33,24 @@ def build(verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(LIB + ".tmp", LIB)
+    build_binding(verbose)
     return LIB
+
+
+def build_binding(verbose: bool = False) -> str:
+    import torch
+    t = os.path.dirname(torch.__file__)
+    cmd = [CXX, "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(x for d in (os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+                         sysconfig.get_paths()["include"]) for x in ("-isystem", d)),
+           "-I", os.path.join(ROOT, "include"), os.path.join(HERE, "csrc", "tq_torch.cpp"), "-o", BINDING + ".tmp",
+           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    os.replace(BINDING + ".tmp", BINDING)
+    return BINDING
 
 
 if __name__ == "__main__":
