@@ -50,12 +50,14 @@ typedef const int32_t __attribute__((address_space(4))) const_i32;
 
 constexpr int kHeads = 16;                 // query heads per work-group (columns of a product)
 constexpr int kRunWaves = 4;               // wavefronts of a work-group that holds a run of steps,
-constexpr int kMostRuns = 2 * 256;         // two such per CU
+constexpr int runs_per_cu(int d) { return d == 256 ? 2 : 3; }   // of which so many fit a CU
 constexpr int kDirectWaves = 8;            // ... that holds one short range
 constexpr int kJoinThreads = 256;
+constexpr int kCus = 256;
 
-// tokens of one step of a wavefront
-constexpr int step_tokens(int d, int bits) { return d * bits >= 1024 ? 32 : 64; }
+// Tokens of one step of a wavefront.  (64 for codes: 98 us instead of 94 for 48
+// streams up to 16384 in 4 bits, with registers for two wavefronts per SIMD only.)
+constexpr int kStep = 32;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -198,9 +200,9 @@ struct Join {
 
 // ---------------------------------------------------------------------------
 template <int W, int D, int BITS, bool BF16>
-__global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) void attend_kernel(const AttendArgs a) {
   constexpr bool DIRECT = W == kDirectWaves;   // one range per work-group
-  constexpr int ST = step_tokens(D, BITS), NT = ST / 16;
+  constexpr int ST = kStep, NT = ST / 16;
   constexpr uint32_t RB = D * BITS / 8;       // bytes of a row
   constexpr int CE = BITS == 16 ? 8 : BITS == 8 ? 16 : (D / 4 < 32 ? D / 4 : 32);  // a lane's run of a key row
   constexpr uint32_t CB = CE * BITS / 8;      // its bytes
@@ -219,6 +221,9 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
   float *const lds_m = lds, *const lds_l = lds + W * kHeads, *const lds_q = lds + 2 * W * kHeads,
                *const lds_o = lds_q + (QL ? KS * 64 * 4 : 0);
 
+  // a wavefront that is behind goes first: wavefronts that progress alike end together
+  // (oldest first, the younger ones are left to themselves at the end)
+  __builtin_amdgcn_s_setprio(3);
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int lps = a.c.lps, hkv = a.c.heads;
@@ -280,9 +285,6 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
       }
   }
   if (x0 >= x1) return;
-  // a wavefront that is behind goes first: wavefronts that progress alike end together
-  // (oldest first, the younger ones are left to themselves at the end)
-  __builtin_amdgcn_s_setprio(3);
   const int quarter = max((x1 - x0) / 4, 1);
 
   for (int x = x0; x < x1;) {
@@ -360,11 +362,11 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
     float s[NT][4];
     // scores, times the keys' scales: row 4 g + j of tile i, head r
     auto scores = [&]() {
+      v4f acc[NT] = {};
 #pragma unroll
-      for (int i = 0; i < NT; i++) {
-        v4f acc = {0, 0, 0, 0};
-#pragma unroll
-        for (int k = 0; k < KS; k++) {
+      for (int n = 0; n < KS * NT; n++) {
+          // (tile by tile at 16 bits; codes, which take longer to prepare, in turn)
+          const int i = BITS == 16 ? n / KS : n % NT, k = BITS == 16 ? n % KS : n / NT;
           u32x4 op;
           if constexpr (BITS == 16) {
             op = u32x4{kraw[i][4 * k], kraw[i][4 * k + 1], kraw[i][4 * k + 2], kraw[i][4 * k + 3]};
@@ -380,11 +382,12 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
             widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
             op = u32x4{y0, y1, y2, y3};
           }
-          acc = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + (k * 64 + lane) * 4) : q[k], acc);
+          acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + (k * 64 + lane) * 4) : q[k], acc[i]);
         }
 #pragma unroll
-        for (int j = 0; j < 4; j++) s[i][j] = BITS < 16 ? fmaf(acc[j], scale_of(ksr[i], j), 0.0f) : acc[j];
-      }
+      for (int i = 0; i < NT; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) s[i][j] = BITS < 16 ? fmaf(acc[i][j], scale_of(ksr[i], j), 0.0f) : acc[i][j];
     };
     // tokens outside the range: no score, and nothing of what their rows hold
     auto masked = [&](int i, int j) -> bool {
@@ -471,45 +474,53 @@ __global__ __launch_bounds__(64 * W, 2) void attend_kernel(const AttendArgs a) {
           const int h = i + j / 2, k = 2 * (j & 1);
           ph[j] = pack2<VBF>(s[h][k], s[h][k + 1]);
           const f2 u = unpack2<VBF>(ph[j]);
-          pl[j] = pack2<VBF>(s[h][k] - u.x, s[h][k + 1] - u.y);
+          pl[j] = pack2<VBF>(fmaf(u.x, -1.0f, s[h][k]), fmaf(u.y, -1.0f, s[h][k + 1]));
         }
-        // rows as 16-bit values, two channels a word: row[tile][j][channel / 2]
-        uint32_t row[2][4][DV / 2];
+        if constexpr (BITS == 16) {
+          // two channels a word: rows 2 j and 2 j + 1 paired up
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+          for (int c = 0; c < DV; c++) {
+            const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+            u32x4 op;
 #pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const uint32_t *raw = vraw[i + h][j];
-            if constexpr (BITS == 16) {
+            for (int j = 0; j < 4; j++)
+              op[j] = __builtin_amdgcn_perm(vraw[i + j / 2][2 * (j & 1) + 1][c / 2], vraw[i + j / 2][2 * (j & 1)][c / 2], sel);
+            o[c] = mfma16<VBF>(op, ph, o[c]);
+            o[c] = mfma16<VBF>(op, pl, o[c]);
+          }
+        } else {
+          // four channels a word of bytes: the bytes paired up, then widened
 #pragma unroll
-              for (int k = 0; k < DV / 2; k++) row[h][j][k] = raw[k];
-            } else if constexpr (BITS == 8) {
+          for (int c = 0; c < DV; c += 4) {
+            u32x4 op[4];
 #pragma unroll
-              for (int k = 0; k < DV / 4; k++) widen4<VBF>(raw[k], 1.0f, row[h][j][2 * k], row[h][j][2 * k + 1]);
-            } else if constexpr (VBr < 4) {
-              // codes 0..3 of the shared word for even lanes, 4..7 for odd ones
-              uint32_t lo, hi;
-              tq4_to_fp8(raw[0], lo, hi);
-              widen4<VBF>(r & 1 ? hi : lo, 512.0f, row[h][j][0], row[h][j][1]);
-            } else {
+            for (int j = 0; j < 4; j++) {
+              uint32_t pair[2];
 #pragma unroll
-              for (int k = 0; k < DV / 8; k++) {
-                uint32_t lo, hi;
-                tq4_to_fp8(raw[k], lo, hi);
-                widen4<VBF>(lo, 512.0f, row[h][j][4 * k], row[h][j][4 * k + 1]);
-                widen4<VBF>(hi, 512.0f, row[h][j][4 * k + 2], row[h][j][4 * k + 3]);
+              for (int k = 0; k < 2; k++) {
+                const uint32_t *raw = vraw[i + j / 2][2 * (j & 1) + k];
+                if constexpr (BITS == 8) {
+                  pair[k] = raw[c / 4];
+                } else {
+                  // a word's codes 0..3, then 4..7; of a word that two lanes share, theirs
+                  uint32_t lo, hi;
+                  tq4_to_fp8(raw[c / 8], lo, hi);
+                  pair[k] = (VBr < 4 ? r & 1 : (c >> 2) & 1) ? hi : lo;
+                }
               }
+              const uint32_t p01 = __builtin_amdgcn_perm(pair[1], pair[0], 0x05010400u);
+              const uint32_t p23 = __builtin_amdgcn_perm(pair[1], pair[0], 0x07030602u);
+              uint32_t w0, w1, w2, w3;
+              widen4<VBF>(p01, BITS == 4 ? 512.0f : 1.0f, w0, w1);
+              widen4<VBF>(p23, BITS == 4 ? 512.0f : 1.0f, w2, w3);
+              op[0][j] = w0; op[1][j] = w1; op[2][j] = w2; op[3][j] = w3;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+              o[c + k] = mfma16<VBF>(op[k], ph, o[c + k]);
+              o[c + k] = mfma16<VBF>(op[k], pl, o[c + k]);
             }
           }
-#pragma unroll
-        for (int c = 0; c < DV; c++) {
-          const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
-          u32x4 op;
-#pragma unroll
-          for (int j = 0; j < 4; j++)
-            op[j] = __builtin_amdgcn_perm(row[j / 2][2 * (j & 1) + 1][c / 2], row[j / 2][2 * (j & 1)][c / 2], sel);
-          o[c] = mfma16<VBF>(op, ph, o[c]);
-          o[c] = mfma16<VBF>(op, pl, o[c]);
         }
       }
     };
@@ -673,9 +684,9 @@ hipError_t go(const AttendArgs &a, hipStream_t s) {
   if (a.direct) return go_attend<kDirectWaves, D, BITS, BF16>(a, s);
   const hipError_t e = go_attend<kRunWaves, D, BITS, BF16>(a, s);
   if (e != hipSuccess) return e;
-  // (about 512 work-groups, or one for every range)
+  // (a head each while that is a few thousand work-groups: those of whole ranges end at once)
   const int vheads = a.c.heads * ((a.group + kHeads - 1) / kHeads), cols = a.group < kHeads ? a.group : kHeads;
-  const int share = 512 / (vheads * a.batch);
+  const int share = 4096 / (vheads * a.batch);
   hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(vheads, a.batch, share < 1 ? 1 : share < cols ? share : cols),
                      dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
@@ -691,17 +702,21 @@ hipError_t go_bits(const AttendArgs &a, bool bf16, hipStream_t s) {
 
 AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window) {
   AttendPlan p;
-  const int group = hq / c.heads, st = step_tokens(c.d, c.bits);
+  const int group = hq / c.heads, st = kStep;
   const int64_t ranges = (int64_t)batch * c.heads * ((group + kHeads - 1) / kHeads);
   // (15 tokens more: a window may start within a tile)
   const int64_t longest = window > 0 && window < max_len ? window + 15 : max_len;
   const int64_t steps = (longest + st - 1) / st;
-  // One work-group per range where that takes two rounds of its wavefronts, or four
-  // if the ranges alone fill the CUs (8 kv heads of 128; graph replays, us, direct
-  // against runs and their join: 1 stream of 512 tokens 8.0 against 8.0, of 1024
-  // 12.1 against 8.4; 32 streams of 1024 22.4 against 29.8; one stream of 1024
-  // among short ones costs 4 more).
-  p.direct = steps <= (ranges >= 256 ? 32 : 16) && ranges < ((int64_t)1 << 31);
+  // One work-group per range where a range is short: up to two rounds of steps of its
+  // wavefronts at 16 bits and 128 channels, up to four of lighter ones, and twice that
+  // where the ranges alone fill half the CUs.  Graph replays, us, direct against runs
+  // and their join (8 kv heads of 128, all streams alike; tokens):
+  //            1 stream                          16 streams
+  //   16 bits  512: 8.0, 8.0   768: 10.0, 8.4    1024: 17.9, 21.2   1536: 28.0, 23.9
+  //    8 bits  768: 8.3, 8.3  1024:  9.7, 8.3    2048: 20.3, 22.4
+  //    4 bits 1024: 8.1, 8.0  1536: 10.2, 8.3    2048: 13.1, 18.6
+  const int rounds2 = 32768 / (c.d * c.bits), most_steps = (rounds2 < 32 ? rounds2 : 32) * (ranges >= kCus / 2 ? 2 : 1);
+  p.direct = steps <= most_steps && ranges < ((int64_t)1 << 31);
   p.steps = ranges * steps;
   if (p.direct) {
     p.blocks = (int)ranges;
@@ -709,7 +724,8 @@ AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int
     return p;
   }
   const int64_t runs = (p.steps + kRunWaves - 1) / kRunWaves;
-  p.blocks = (int)(runs < kMostRuns ? runs : kMostRuns);
+  const int most = kCus * runs_per_cu(c.d);
+  p.blocks = (int)(runs < most ? runs : most);
   p.scratch = (size_t)p.blocks * 2 * part_floats(c.d, group < kHeads ? group : kHeads) * 4 + (size_t)ranges * sizeof(Join);
   return p;
 }
