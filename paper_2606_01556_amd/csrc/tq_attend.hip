@@ -48,7 +48,7 @@ typedef float f2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef const int32_t __attribute__((address_space(4))) const_i32;
 
-constexpr int kHeads = 16;                 // query heads per work-group (columns of a product)
+constexpr int kHeads = 16;                 // query heads of a product (its columns)
 constexpr int kRunWaves = 4;               // wavefronts of a work-group that holds a run of steps,
 constexpr int runs_per_cu(int d) { return d == 256 ? 2 : 3; }   // of which so many fit a CU
 constexpr int kDirectWaves = 8;            // ... that holds one short range
@@ -58,6 +58,12 @@ constexpr int kCus = 256;
 // Tokens of one step of a wavefront.  (64 for codes: 98 us instead of 94 for 48
 // streams up to 16384 in 4 bits, with registers for two wavefronts per SIMD only.)
 constexpr int kStep = 32;
+
+// A kv head's group of query heads is one range of one or two blocks of up to 16 heads,
+// or, past 32 heads, several ranges.
+__host__ __device__ constexpr int head_blocks(int group) { return group > kHeads ? 2 : 1; }
+constexpr int ranges_of(int group) { return (group + kHeads * head_blocks(group) - 1) / (kHeads * head_blocks(group)); }
+constexpr int range_heads(int group) { return group < kHeads * head_blocks(group) ? group : kHeads * head_blocks(group); }
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -97,24 +103,25 @@ __device__ __forceinline__ f2 unpack2(uint32_t w) {
 
 // NB bytes from p (p aligned to min(NB, 16)).  The cache is read once per call:
 // non-temporal loads stream it at 7.0 TB/s instead of 6.2 (512 MB).
-template <typename T>
+template <bool ONCE, typename T>
 __device__ __forceinline__ T stream_load(const uint8_t *p) {
-  return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
+  else return *reinterpret_cast<const T *>(p);
 }
-template <int NB>
+template <bool ONCE, int NB>
 __device__ __forceinline__ void load_bytes(const uint8_t *p, uint32_t *out) {
   if constexpr (NB >= 16) {
 #pragma unroll
     for (int i = 0; i < NB / 16; i++) {
-      const u32x4 v = stream_load<u32x4>(p + 16 * i);
+      const u32x4 v = stream_load<ONCE, u32x4>(p + 16 * i);
       out[4 * i] = v.x; out[4 * i + 1] = v.y; out[4 * i + 2] = v.z; out[4 * i + 3] = v.w;
     }
   } else if constexpr (NB == 8) {
-    const u32x2 v = stream_load<u32x2>(p);
+    const u32x2 v = stream_load<ONCE, u32x2>(p);
     out[0] = v.x; out[1] = v.y;
   } else {
     static_assert(NB == 4);
-    out[0] = stream_load<uint32_t>(p);
+    out[0] = stream_load<ONCE, uint32_t>(p);
   }
 }
 
@@ -176,10 +183,10 @@ __host__ __device__ constexpr int part_floats(int d, int cols) { return part_hea
 // Q in LDS instead of registers, which 16-bit rows of 256 values leave none for
 constexpr bool q_in_lds(int d, int bits) { return d == 256 && bits == 16; }
 
-// floats of LDS: [W][kHeads] references and sums, Q where it is there, then [W][cols]
-// [d + 4] products (rows staggered over the banks)
-constexpr int lds_floats(int waves, int d, int bits, int cols) {
-  return 2 * waves * kHeads + (q_in_lds(d, bits) ? d / 32 * 64 * 4 : 0) + waves * cols * (d + 4);
+// floats of LDS: [W][kHeads] references and sums, Q where it is there, then [W][cols up
+// to kHeads][d + 4] products (rows staggered over the banks)
+constexpr int lds_floats(int waves, int hb, int d, int bits, int cols) {
+  return 2 * waves * kHeads + (q_in_lds(d, bits) ? hb * (d / 32) * 64 * 4 : 0) + waves * cols * (d + 4);
 }
 
 // a head's four output values from d0, and its log-sum-exp
@@ -199,9 +206,12 @@ struct Join {
 };
 
 // ---------------------------------------------------------------------------
-template <int W, int D, int BITS, bool BF16>
+// HB: blocks of up to 16 query heads per range.  With two, half of the wavefronts take
+// each, step by step alongside, so that the cache is read from memory once.
+template <int W, int HB, int D, int BITS, bool BF16>
 __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) void attend_kernel(const AttendArgs a) {
   constexpr bool DIRECT = W == kDirectWaves;   // one range per work-group
+  constexpr int SW = W / HB, HR = kHeads * HB; // wavefronts that share a block's steps; heads of a range
   constexpr int ST = kStep, NT = ST / 16;
   constexpr uint32_t RB = D * BITS / 8;       // bytes of a row
   constexpr int CE = BITS == 16 ? 8 : BITS == 8 ? 16 : (D / 4 < 32 ? D / 4 : 32);  // a lane's run of a key row
@@ -219,7 +229,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 
   extern __shared__ __attribute__((aligned(16))) float lds[];
   float *const lds_m = lds, *const lds_l = lds + W * kHeads, *const lds_q = lds + 2 * W * kHeads,
-               *const lds_o = lds_q + (QL ? KS * 64 * 4 : 0);
+               *const lds_o = lds_q + (QL ? HB * KS * 64 * 4 : 0);
 
   // a wavefront that is behind goes first: wavefronts that progress alike end together
   // (oldest first, the younger ones are left to themselves at the end)
@@ -228,8 +238,9 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
   const int r = lane & 15, g = lane >> 4;
   const int lps = a.c.lps, hkv = a.c.heads;
   const int cap = a.max_pages << lps;
-  const int hblocks = (a.group + kHeads - 1) / kHeads, vheads = hkv * hblocks;
-  const int cols = min(a.group, kHeads);
+  const int hblocks = (a.group + HR - 1) / HR, vheads = hkv * hblocks;
+  const int cols = min(a.group, HR), wcols = min(a.group, kHeads);
+  const int wb = w / SW, ws = w % SW;          // the wavefront's block of heads and its turn
 
   // this work-group's run of steps
   int b, vh, t, x0, x1, chunk;
@@ -275,8 +286,8 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       for (int e = threadIdx.x; e < rows; e += 64 * W) a.lse[row0 + e] = -INFINITY;
   };
   if constexpr (DIRECT) {
-    const int h0 = vh % hblocks * kHeads;
-    if (x1 == 0) clear((int64_t)b * a.hq + vh / hblocks * a.group + h0, min(kHeads, a.group - h0));
+    const int h0 = vh % hblocks * HR;
+    if (x1 == 0) clear((int64_t)b * a.hq + vh / hblocks * a.group + h0, min(HR, a.group - h0));
   } else {
     for (int i = blockIdx.x; i < a.batch; i += gridDim.x)
       if (range_of<ST>(uniform(a.lengths[i]), cap, a.window).steps == 0) {
@@ -289,8 +300,8 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 
   for (int x = x0; x < x1;) {
     const int n = min(rg.steps - t, x1 - x);
-    const int kvh = vh / hblocks, hb = vh % hblocks;
-    const int heads = min(kHeads, a.group - hb * kHeads);   // live columns
+    const int kvh = vh / hblocks, h0 = vh % hblocks * HR;
+    const int heads = max(0, min(kHeads, a.group - h0 - wb * kHeads));   // live columns
 
     const_i32 *pages = (const_i32 *)(a.table + b * a.table_stride);
     const int last_page = (rg.len - 1) >> lps;
@@ -309,7 +320,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       for (int i = 0; i < NT; i++) {
         const uint8_t *kp = a.c.k + row[i] * RB;
 #pragma unroll
-        for (int j = 0; j < KL; j++) load_bytes<CB>(kp + j * 4 * CB + kofs, &kraw[i][j * (int)CB / 4]);
+        for (int j = 0; j < KL; j++) load_bytes<HB == 1, CB>(kp + j * 4 * CB + kofs, &kraw[i][j * (int)CB / 4]);
         if constexpr (BITS < 16)
           ksr[i] = *reinterpret_cast<const u32x2 *>(reinterpret_cast<const uint8_t *>(a.c.ks + row[i]) + sofs);
       }
@@ -323,13 +334,13 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       for (int i = 0; i < NT; i++) {
         const uint8_t *vp = a.c.v + row[i] * RB;
 #pragma unroll
-        for (int j = 0; j < 4; j++) load_bytes<VB>(vp + j * RB + vofs, vraw[i][j]);
+        for (int j = 0; j < 4; j++) load_bytes<HB == 1, VB>(vp + j * RB + vofs, vraw[i][j]);
       }
     };
 
-    // the wavefront's steps t + w, t + w + W, ... of the range
-    int t0 = uniform(rg.base + (t + w) * ST);
-    const int steps = (n - w + W - 1) / W;
+    // the wavefront's steps t + ws, t + ws + SW, ... of the range
+    int t0 = uniform(rg.base + (t + ws) * ST);
+    const int steps = (n - ws + SW - 1) / SW;
     int64_t row[NT];
     if (steps > 0) {
 #pragma unroll
@@ -343,15 +354,15 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     u32x4 q[KS];
     const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);     // (-infinity times it has to stay so)
     {
-      const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + hb * kHeads + min(r, heads - 1)) * a.q_hs;
+      const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + h0 + min(wb * kHeads + r, a.group - h0 - 1)) * a.q_hs;
       const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, live = r < heads ? 0xffffffffu : 0u;
 #pragma unroll
       for (int k = 0; k < KS; k++) {
-        if (QL && k % W != w) continue;
+        if (QL && k % SW != ws) continue;
         q[k] = *reinterpret_cast<const u32x4 *>(qp + (8 * k / CE) * 4 * CE + g * CE + 8 * k % CE);
 #pragma unroll
         for (int i = 0; i < 4; i++) q[k][i] = (q[k][i] ^ flip) & live;
-        if constexpr (QL) *reinterpret_cast<u32x4 *>(lds_q + (k * 64 + lane) * 4) = q[k];
+        if constexpr (QL) *reinterpret_cast<u32x4 *>(lds_q + ((wb * KS + k) * 64 + lane) * 4) = q[k];
       }
       if constexpr (QL) __syncthreads();
     }
@@ -382,7 +393,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
             widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
             op = u32x4{y0, y1, y2, y3};
           }
-          acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + (k * 64 + lane) * 4) : q[k], acc[i]);
+          acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + ((wb * KS + k) * 64 + lane) * 4) : q[k], acc[i]);
         }
 #pragma unroll
       for (int i = 0; i < NT; i++)
@@ -531,12 +542,12 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     if (steps > 0) {
       int ahead[NT];
 #pragma unroll
-      for (int i = 0; i < NT; i++) ahead[i] = page_of(t0 + W * ST + 16 * i);
+      for (int i = 0; i < NT; i++) ahead[i] = page_of(t0 + SW * ST + 16 * i);
       for (int u = 0; u < steps - 1; u++) {
 #pragma unroll
         for (int i = 0; i < NT; i++) {
-          row[i] = row_of(ahead[i], t0 + W * ST + 16 * i);
-          ahead[i] = page_of(t0 + 2 * W * ST + 16 * i);
+          row[i] = row_of(ahead[i], t0 + SW * ST + 16 * i);
+          ahead[i] = page_of(t0 + 2 * SW * ST + 16 * i);
         }
         scores();
         load_k(row);
@@ -545,8 +556,8 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
         if (t0 < rg.first) mask_values();
         products();
         load_v(row);
-        t0 += W * ST;
-        const int done = x - x0 + W * u;
+        t0 += SW * ST;
+        const int done = x - x0 + SW * u;
         if (done >= quarter) {
           if (done < 2 * quarter) __builtin_amdgcn_s_setprio(2);
           else if (done < 3 * quarter) __builtin_amdgcn_s_setprio(1);
@@ -573,31 +584,32 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       for (int i = 0; i < 4; i++)
 #pragma unroll
         for (int c = 0; c < DV; c += 4)
-          *reinterpret_cast<v4f *>(&lds_o[(w * cols + r) * LD + DV * (4 * g + i) + c]) =
+          *reinterpret_cast<v4f *>(&lds_o[(w * wcols + r) * LD + DV * (4 * g + i) + c]) =
               v4f{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
     }
     __syncthreads();
     const bool whole = n == rg.steps;
-    const int64_t row0 = (int64_t)b * a.hq + kvh * a.group + hb * kHeads;
+    const int64_t row0 = (int64_t)b * a.hq + kvh * a.group + h0;
     const int slot = 2 * blockIdx.x + (x == x0 ? 0 : 1);
     float *part = parts + (int64_t)slot * part_floats(D, cols);
     if (!DIRECT && t == 0 && threadIdx.x == 0) {
       const int end = x + rg.steps - 1;      // the range's last step
       joins[(int64_t)b * vheads + vh] = Join{slot, whole ? 0 : end / chunk - (int)blockIdx.x + 1};
     }
-    for (int e = threadIdx.x; e < heads * (D / 4); e += 64 * W) {
+    for (int e = threadIdx.x; e < min(cols, a.group - h0) * (D / 4); e += 64 * W) {
       const int h = e / (D / 4), d0 = 4 * (e % (D / 4));
-      float mm = lds_m[h];
+      const int first = h / kHeads * SW, c = h % kHeads;    // its wavefronts, its column
+      float mm = lds_m[first * kHeads + c];
 #pragma unroll
-      for (int i = 1; i < W; i++) mm = fmaxf(mm, lds_m[i * kHeads + h]);
+      for (int i = 1; i < SW; i++) mm = fmaxf(mm, lds_m[(first + i) * kHeads + c]);
       const float ref = mm == -INFINITY ? 0.0f : mm;
       float ll = 0.0f;
       v4f y = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < W; i++) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[i * kHeads + h] - ref);
-        const v4f z = *reinterpret_cast<const v4f *>(&lds_o[(i * cols + h) * LD + d0]);
-        ll = fmaf(f, lds_l[i * kHeads + h], ll);
+      for (int i = 0; i < SW; i++) {
+        const float f = __builtin_amdgcn_exp2f(lds_m[(first + i) * kHeads + c] - ref);
+        const v4f z = *reinterpret_cast<const v4f *>(&lds_o[((first + i) * wcols + c) * LD + d0]);
+        ll = fmaf(f, lds_l[(first + i) * kHeads + c], ll);
 #pragma unroll
         for (int k = 0; k < 4; k++) y[k] = fmaf(f, z[k], y[k]);
       }
@@ -632,12 +644,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendArgs a) 
   constexpr int Q = D / 4, GROUPS = kJoinThreads / Q;
   __shared__ __attribute__((aligned(16))) float lds_o[GROUPS][D], lds_ml[GROUPS][2];
   const int b = blockIdx.y, vh = blockIdx.x, vheads = gridDim.x;
-  const int hblocks = (a.group + kHeads - 1) / kHeads, cols = min(a.group, kHeads);
+  const int hr = kHeads * head_blocks(a.group), hblocks = (a.group + hr - 1) / hr, cols = min(a.group, hr);
   const Join *joins = reinterpret_cast<const Join *>(a.scratch + (int64_t)a.blocks * 2 * part_floats(D, cols));
   const Join j = joins[(int64_t)b * vheads + vh];
   if (j.parts == 0) return;                      // written by its work-group
-  const int kvh = vh / hblocks, hb = vh % hblocks;
-  const int heads = min(kHeads, a.group - hb * kHeads);
+  const int kvh = vh / hblocks, h0 = vh % hblocks * hr;
+  const int heads = min(hr, a.group - h0);
   const int pg = threadIdx.x / Q, d0 = 4 * (threadIdx.x % Q);
   for (int h = blockIdx.z; h < heads; h += gridDim.z) {
     float m = -INFINITY, l = 0.0f;
@@ -664,29 +676,28 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendArgs a) 
     if (pg == 0) {
 #pragma unroll
       for (int k = 1; k < GROUPS; k++) add(*reinterpret_cast<const f2 *>(lds_ml[k]), *reinterpret_cast<const v4f *>(&lds_o[k][d0]));
-      store4<BF16>(a, D, (int64_t)b * a.hq + kvh * a.group + hb * kHeads + h, d0, m, l, o);
+      store4<BF16>(a, D, (int64_t)b * a.hq + kvh * a.group + h0 + h, d0, m, l, o);
     }
     __syncthreads();
   }
 }
 
-template <int W, int D, int BITS, bool BF16>
+template <int W, int HB, int D, int BITS, bool BF16>
 hipError_t go_attend(const AttendArgs &a, hipStream_t s) {
-  const int cols = a.group < kHeads ? a.group : kHeads;
-  const int bytes = lds_floats(W, D, BITS, cols) * 4;
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(attend_kernel<W, D, BITS, BF16>), bytes);
+  const int bytes = lds_floats(W, HB, D, BITS, a.group < kHeads ? a.group : kHeads) * 4;
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(attend_kernel<W, HB, D, BITS, BF16>), bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attend_kernel<W, D, BITS, BF16>), dim3(a.blocks), dim3(64 * W), bytes, s, a);
+  hipLaunchKernelGGL((attend_kernel<W, HB, D, BITS, BF16>), dim3(a.blocks), dim3(64 * W), bytes, s, a);
   return hipGetLastError();
 }
 template <int D, int BITS, bool BF16>
 hipError_t go(const AttendArgs &a, hipStream_t s) {
-  if (a.direct) return go_attend<kDirectWaves, D, BITS, BF16>(a, s);
-  const hipError_t e = go_attend<kRunWaves, D, BITS, BF16>(a, s);
+  const bool two = head_blocks(a.group) == 2;
+  if (a.direct) return two ? go_attend<kDirectWaves, 2, D, BITS, BF16>(a, s) : go_attend<kDirectWaves, 1, D, BITS, BF16>(a, s);
+  const hipError_t e = two ? go_attend<kRunWaves, 2, D, BITS, BF16>(a, s) : go_attend<kRunWaves, 1, D, BITS, BF16>(a, s);
   if (e != hipSuccess) return e;
   // (a head each while that is a few thousand work-groups: those of whole ranges end at once)
-  const int vheads = a.c.heads * ((a.group + kHeads - 1) / kHeads), cols = a.group < kHeads ? a.group : kHeads;
-  const int share = 4096 / (vheads * a.batch);
+  const int vheads = a.c.heads * ranges_of(a.group), cols = range_heads(a.group), share = 4096 / (vheads * a.batch);
   hipLaunchKernelGGL((join_kernel<D, BF16>), dim3(vheads, a.batch, share < 1 ? 1 : share < cols ? share : cols),
                      dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
@@ -703,7 +714,7 @@ hipError_t go_bits(const AttendArgs &a, bool bf16, hipStream_t s) {
 AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window) {
   AttendPlan p;
   const int group = hq / c.heads, st = kStep;
-  const int64_t ranges = (int64_t)batch * c.heads * ((group + kHeads - 1) / kHeads);
+  const int64_t ranges = (int64_t)batch * c.heads * ranges_of(group);
   // (15 tokens more: a window may start within a tile)
   const int64_t longest = window > 0 && window < max_len ? window + 15 : max_len;
   const int64_t steps = (longest + st - 1) / st;
@@ -726,7 +737,7 @@ AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int
   const int64_t runs = (p.steps + kRunWaves - 1) / kRunWaves;
   const int most = kCus * runs_per_cu(c.d);
   p.blocks = (int)(runs < most ? runs : most);
-  p.scratch = (size_t)p.blocks * 2 * part_floats(c.d, group < kHeads ? group : kHeads) * 4 + (size_t)ranges * sizeof(Join);
+  p.scratch = (size_t)p.blocks * 2 * part_floats(c.d, range_heads(group)) * 4 + (size_t)ranges * sizeof(Join);
   return p;
 }
 

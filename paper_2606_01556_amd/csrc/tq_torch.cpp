@@ -141,6 +141,7 @@ void *to_stream(PyObject *o) {
 struct Cache {
   tq_kv_cache c;
   int64_t device;
+  at::Tensor kept[4];    // k, v, k_scales, v_scales
 };
 const char *const kCapsule = "tq_kv_cache";
 
@@ -149,6 +150,15 @@ const Cache &cache_of(PyObject *o, int64_t device) {
   if (c == nullptr) throw Failed();
   if (c->device != device)
     fail(PyExc_ValueError, "cache: on device %d, but the current device is %d", (int)c->device, (int)device);
+  // (a tensor's memory can be exchanged or resized under it)
+  const void *const at[4] = {c->c.k, c->c.v, c->c.k_scales, c->c.v_scales};
+  const int64_t places = (int64_t)c->c.pages * c->c.kv_heads * c->c.page_size;
+  for (int i = 0; i < (c->c.bits == 16 ? 2 : 4); i++) {
+    const at::Tensor &t = c->kept[i];
+    const int64_t row = i >= 2 ? 1 : c->c.bits == 4 ? c->c.head_dim / 8 : c->c.head_dim;
+    if (t.numel() != places * row || t.data_ptr() != at[i])
+      fail(PyExc_ValueError, "cache: its tensors were moved or resized; make a new KVCache of them");
+  }
   return *c;
 }
 // a row's type next to the cache's
@@ -188,6 +198,7 @@ PyObject *make_cache(PyObject *const *a, Py_ssize_t) {
   c.c.head_dim = (int32_t)d;
   c.c.bits = bits;
   c.c.dtype = type == at::kBFloat16 ? TQ_BF16 : TQ_F16;
+  for (int i = 0; i < (bits == 16 ? 2 : 4); i++) c.kept[i] = THPVariable_Unpack(a[i]);
   Cache *kept = new Cache(c);
   PyObject *handle = PyCapsule_New(kept, kCapsule, [](PyObject *o) {
     delete static_cast<Cache *>(PyCapsule_GetPointer(o, kCapsule));

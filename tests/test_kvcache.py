@@ -243,6 +243,10 @@ def test_binding_refuses():
         tq.KVCache(c16.k, c16.v, c4.k_scales, c4.v_scales)
     with pytest.raises(AttributeError):
         c16.k = c16.v
+    moved = tq.empty_kv_cache(4, 16, 2, 128)
+    moved.v.data = moved.v.clone()
+    with pytest.raises(ValueError):
+        tq.kv_append(moved, k, k, slots)
     for bad in (new(3, 3, 128), new(3, 2, 64), new(2, 2, 128), new(3, 2, 256)[..., ::2], new(3, 2 * 132)[:, :264].view(3, 2, 132)[..., 4:],
                 k.cpu(), new(3, 256)):
         with pytest.raises(ValueError):
@@ -542,6 +546,17 @@ def test_attention_lengths(kind, dtype, d, heads, group, page):
     say("attend", kind, dtype, d, heads, group, page)
     s = Streams(LENS, heads, d, page, kind, dtype, seed=d)
     attend(s, randn(len(LENS), heads * group, d, seed=5, scale=1.5).to(dtype))
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("group", [17, 31, 32, 33, 40, 70])
+@pytest.mark.parametrize("d,lens", [(64, [0, 40, 300]), (128, [1, 129]), (128, [5000, 0, 33]), (256, [600]), (256, [4100])])
+def test_attention_wide_groups(kind, dtype, group, d, lens):
+    """More query heads to a key-value head than a product has columns."""
+    say("wide", kind, dtype, group, d, lens)
+    s = Streams(lens, 2, d, 16, kind, dtype, seed=group)
+    attend(s, randn(len(lens), 2 * group, d, seed=5, scale=1.5).to(dtype))
 
 
 @gpu
