@@ -3,10 +3,10 @@
 //
 // All three are one pass over head rows of d = 64, 128 or 256 16-bit values and
 // bound by memory.  d / 16 lanes own a row, each two runs of eight values (16
-// bytes).  Where a row is rotated by halves, the runs are 8 e .. 8 e + 7 and
-// rot / 2 + 8 e .. + 7, so both values of every rotated pair are in one lane; the
-// row's sum of squares and largest value come from DPP lane swaps among its
-// lanes.  Nothing passes through LDS, and a row is read and written once.
+// bytes), half of the rotated channels apart, so that both values of every rotated
+// pair are in one lane whichever way they are paired; the row's sum of squares and
+// largest value come from DPP lane swaps among its lanes.  Nothing passes through
+// LDS, and a row is read and written once.
 #include "tq_device.hpp"
 #include "tq_kv.hpp"
 
@@ -112,11 +112,12 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
   const int kind = r < a.hq ? 0 : r < a.hq + a.hkv ? 1 : 2;
   const int head = kind == 0 ? r : kind == 1 ? r - a.hq : r - a.hq - a.hkv;
   const HeadRows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-  // the lane's two runs of eight values
+  // the lane's two runs of eight values, in the two halves of the rotated channels or
+  // of the others: either is a stretch that neighbouring lanes continue (two runs side
+  // by side: 24 us instead of 22 for 8192 tokens in 8 bits, written and read back)
   const bool turned = e < a.rot / 16;
-  const bool halves = turned && !a.interleaved;
-  const int i0 = halves ? 8 * e : 16 * e;
-  const int i1 = halves ? a.rot / 2 + 8 * e : 16 * e + 8;
+  const int i0 = 8 * e + (turned ? 0 : a.rot / 2);
+  const int i1 = 8 * e + (turned ? a.rot / 2 : D / 2);
   const uint16_t *p = src.p + (int64_t)token * src.ts + head * src.hs;
   const u32x4 r0 = *reinterpret_cast<const u32x4 *>(p + i0);
   const u32x4 r1 = *reinterpret_cast<const u32x4 *>(p + i1);
@@ -135,11 +136,13 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
   if (turn) {
     int pos = a.positions[token];
     pos = min(max(pos, 0), a.max_pos - 1);
-    const float *t = a.table + (int64_t)pos * a.rot + 8 * e;
+    // angles of pairs 8 e .. 8 e + 7, or of those in the two runs
+    const float *t = a.table + (int64_t)pos * a.rot;
+    const int at[2] = {a.interleaved ? 4 * e : 8 * e, a.interleaved ? a.rot / 4 + 4 * e : 8 * e + 4};
 #pragma unroll
     for (int i = 0; i < 2; i++) {
-      const v4f c = *reinterpret_cast<const v4f *>(t + 4 * i);
-      const v4f s = *reinterpret_cast<const v4f *>(t + a.rot / 2 + 4 * i);
+      const v4f c = *reinterpret_cast<const v4f *>(t + at[i]);
+      const v4f s = *reinterpret_cast<const v4f *>(t + a.rot / 2 + at[i]);
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         cs[4 * i + j] = c[j];
