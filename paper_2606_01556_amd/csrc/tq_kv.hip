@@ -65,6 +65,13 @@ __device__ __forceinline__ u32x4 narrow(const float *v) {
   return r;
 }
 
+// a b + c d to within about an ulp also where the products cancel: the rounding of
+// the second is found by an fma and added back (Kahan's difference of products).
+__device__ __forceinline__ float two_products(float a, float b, float c, float d) {
+  const float w = c * d;
+  return fmaf(a, b, w) + fmaf(c, d, -w);
+}
+
 // e4m3 codes of eight values over their scale: clamp(v / s), rounded half to
 // even.  y = 1 / s to within an ulp or two; t = v y is put right by its exact
 // remainder, so that a quotient on a rounding boundary of e4m3 (at most five
@@ -167,15 +174,15 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const float x = v[2 * i], y = v[2 * i + 1];
-        v[2 * i] = x * cs[i] - y * cs[8 + i];
-        v[2 * i + 1] = y * cs[i] + x * cs[8 + i];
+        v[2 * i] = two_products(x, cs[i], -y, cs[8 + i]);
+        v[2 * i + 1] = two_products(y, cs[i], x, cs[8 + i]);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const float x = v[i], y = v[8 + i];
-        v[i] = x * cs[i] - y * cs[8 + i];
-        v[8 + i] = y * cs[i] + x * cs[8 + i];
+        v[i] = two_products(x, cs[i], -y, cs[8 + i]);
+        v[8 + i] = two_products(y, cs[i], x, cs[8 + i]);
       }
     }
   }
