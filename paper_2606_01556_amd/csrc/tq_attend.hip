@@ -6,14 +6,11 @@
 // group), so the kernel is built around one pass over them with nothing but
 // registers between memory and the matrix cores:
 //
-//  * S^T = K Q^T with the group's query heads (up to 16) as columns.  A lane of the
-//    first operand holds values of one token's key, a run of the cache row as it
-//    lies in memory: which of a row's values make up one product is free as long as
-//    Q is laid out alike, so each format loads the widest run a lane can.  16-bit
-//    rows enter 16x16x32 products as they are.  Codes (d >= 128) enter 16x16x128
-//    products as e4m3 bytes, also as they are: Q is split into e4m3 terms instead,
-//    each 2^-4 of the one before, three for fp16 and two for bf16, which hold its
-//    significand exactly.
+//  * S^T = K Q^T in 16x16x32 products, with the group's query heads (up to 16) as
+//    columns.  A lane of the first operand holds values of one token's key, a run of
+//    the cache row as it lies in memory: which of a row's values make up one product
+//    is free as long as Q is laid out alike, so each format loads the widest run a lane
+//    can.  Codes are widened to Q's type (exactly) on their way.
 //  * The result has column lane % 16 and rows 4 (lane / 16) + i: a lane holds the
 //    scores of one head for tokens 4 g + i.  Two such tiles, exponentiated, are
 //    the second operand of O^T = V^T P^T as they stand (the order of the tokens
@@ -24,14 +21,32 @@
 //    quantized row is part of its weight.
 //  * The softmax's reference (and with it the scaling of the weights) only moves
 //    when some weight passes 2^8: most steps have no exchange between lanes and no
-//    rescaling.  Weights in fp16 then keep 11 bits down to 2^-22 of the largest.
+//    rescaling.  A weight enters the products as two 16-bit terms, its rounded value
+//    and what that leaves (fp16 terms for codes and fp16 rows, bf16 ones for bf16
+//    rows): the matrix cores have the time, and one term alone would put 2^-9 of bf16
+//    into every weight.
 //
 // The work is cut evenly whatever the lengths: all (stream, head) ranges of steps
-// laid end to end are split into equal runs, one per work-group, and a work-group's
-// eight wavefronts take its steps in turn.  A range that one run holds whole is
-// written at once; a second launch joins the parts of the others, in their order, so
-// that a result does not depend on timing.  Short ranges get a work-group each and
-// need no second launch.
+// laid end to end are split into equal runs, three work-groups a CU, and a
+// work-group's four wavefronts take its steps in turn.  A range that one run holds
+// whole is written at once; a second launch joins the parts of the others, in their
+// order, so that a result does not depend on timing.  Short ranges get a work-group
+// each and need no second launch.
+//
+// Measured (d = 128, both launches, back-to-back calls; reading alone streams 512 MB at
+// 7.0 TB/s):
+//   1 stream of 131072 tokens, 8 kv heads, fp16              88 us, 6.1 TB/s
+//   32 streams up to 8192, bf16                              95 us, 6.1 TB/s
+//   64 streams up to 8192, 8 bits, pages of 64              101 us, 5.8 TB/s
+//   48 streams up to 16384, 4 bits, pages of 16              85 us, 5.2 TB/s
+// of which the first launch keeps the memory busy for 80, 88, 91 and 75 us (6.5 TB/s
+// and more, 4 bits with their scales' 32-byte runs), the ends of the work-groups are 4
+// to 5 apart, and the join takes 4 to 6.  At 4 bits the vector ALU is 55 % busy, at 16
+// bits 9 %.  Without effect or worse: e4m3 products of the keys with Q split into e4m3
+// terms (and scores off by 2^-15 of sum |q k|), eight wavefronts in one work-group, a
+// join by whichever work-group comes last (its fences drop the L2s under the others).
+#include <cfloat>
+
 #include "tq_device.hpp"
 #include "tq_kernels.hpp"
 #include "tq_kv.hpp"
@@ -147,34 +162,17 @@ __device__ __forceinline__ Range range_of(int len, int cap, int window) {
   return r;
 }
 
-// steps of streams b0 + lane, summed over the lanes up to this one
-template <int ST>
-__device__ __forceinline__ int scan64(const AttendArgs &a, int cap, int b0) {
-  const int lane = threadIdx.x & 63, b = b0 + lane;
-  int incl = b < a.batch ? range_of<ST>(a.lengths[b], cap, a.window).steps : 0;
+// v summed over the lanes up to this one
+__device__ __forceinline__ int scan64(int v) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(incl, m);
-    if (lane >= m) incl += o;
+    const int o = __shfl_up(v, m);
+    if (lane >= m) v += o;
   }
-  return incl;
+  return v;
 }
-
-// How the call's steps are cut: run w holds steps [w chunk, (w + 1) chunk) of all
-// ranges laid end to end, of every stream's `vheads` ranges in turn.
-struct Cut {
-  int total, chunk;
-};
-template <int ST>
-__device__ Cut cut_of(const AttendArgs &a, int cap, int vheads, int runs, int &first64) {
-  Cut c;
-  first64 = scan64<ST>(a, cap, 0);
-  int sum = uniform(__shfl(first64, 63));
-  for (int b0 = 64; b0 < a.batch; b0 += 64) sum += uniform(__shfl(scan64<ST>(a, cap, b0), 63));
-  c.total = sum * vheads;                       // < 2^31 (host)
-  c.chunk = max((c.total + runs - 1) / runs, kRunWaves);
-  return c;
-}
+__device__ __forceinline__ int lane_of(int v, int lane) { return uniform(__shfl(v, lane)); }
 
 // floats of one part of a range: the group's references and sums, then its products
 __host__ __device__ constexpr int part_head(int cols) { return (2 * cols + 3) & ~3; }
@@ -252,26 +250,38 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     t = x0 = 0;
     x1 = chunk = rg.steps;
   } else {
-    int first64;
-    const Cut cut = cut_of<ST>(a, cap, vheads, gridDim.x, first64);
-    chunk = cut.chunk;
+    // Run w holds steps [w chunk, (w + 1) chunk) of all ranges laid end to end, those of
+    // every stream's vheads ranges in turn.  A lane adds up `each` streams.
+    auto steps_of = [&](int i, int end) -> int { return i < end ? range_of<ST>(a.lengths[i], cap, a.window).steps : 0; };
+    const int each = (a.batch + 63) / 64;
+    int mine = 0;
+#pragma unroll 4
+    for (int i = 0; i < each; i++) mine += steps_of(lane * each + i, a.batch);
+    int upto = scan64(mine);
+    const int total = lane_of(upto, 63) * vheads;        // < 2^31 (host)
+    chunk = max((total + (int)gridDim.x - 1) / (int)gridDim.x, kRunWaves);
     x0 = blockIdx.x * chunk;
-    x1 = min(cut.total, x0 + chunk);
+    x1 = min(total, x0 + chunk);
     b = 0;
     vh = t = 0;
     if (x0 < x1) {
       // the stream that holds step x0: the first whose steps end past it
       const int y = x0 / vheads;
-      int before = 0, incl = first64, b0 = 0;
-      uint64_t past;
-      while ((past = __ballot(before + incl > y)) == 0) {
-        before += uniform(__shfl(incl, 63));
-        b0 += 64;
-        incl = scan64<ST>(a, cap, b0);
+      int before = 0, at = __builtin_ctzll(__ballot(upto > y));
+      if (at > 0) before = lane_of(upto, at - 1);
+      b = at * each;
+      if (each > 1) {
+        const int end = min(a.batch, b + each);
+        uint64_t past;
+        while ((past = __ballot(before + (upto = scan64(steps_of(b + lane, end))) > y)) == 0) {
+          before += lane_of(upto, 63);
+          b += 64;
+        }
+        at = __builtin_ctzll(past);
+        if (at > 0) before += lane_of(upto, at - 1);
+        b += at;
       }
-      const int at = __builtin_ctzll(past);
-      b = uniform(b0 + at);
-      before += at == 0 ? 0 : uniform(__shfl(incl, at - 1));
+      b = uniform(b);
       rg = range_of<ST>(uniform(a.lengths[b]), cap, a.window);
       vh = (x0 - before * vheads) / rg.steps;
       t = (x0 - before * vheads) % rg.steps;
@@ -369,32 +379,34 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     v4f o[DV];
 #pragma unroll
     for (int i = 0; i < DV; i++) o[i] = v4f{0, 0, 0, 0};
-    float m = -INFINITY, l = 0.0f;
+    // (finite, so that keys whose score is -infinity have the weight 0 also before the
+    // first finite one)
+    float m = -FLT_MAX, l = 0.0f;
     float s[NT][4];
     // scores, times the keys' scales: row 4 g + j of tile i, head r
     auto scores = [&]() {
       v4f acc[NT] = {};
 #pragma unroll
-      for (int n = 0; n < KS * NT; n++) {
-          // (tile by tile at 16 bits; codes, which take longer to prepare, in turn)
-          const int i = BITS == 16 ? n / KS : n % NT, k = BITS == 16 ? n % KS : n / NT;
-          u32x4 op;
-          if constexpr (BITS == 16) {
-            op = u32x4{kraw[i][4 * k], kraw[i][4 * k + 1], kraw[i][4 * k + 2], kraw[i][4 * k + 3]};
+      for (int e = 0; e < KS * NT; e++) {
+        // (tile by tile at 16 bits; codes, which take longer to prepare, in turn)
+        const int i = BITS == 16 ? e / KS : e % NT, k = BITS == 16 ? e % KS : e / NT;
+        u32x4 op;
+        if constexpr (BITS == 16) {
+          op = u32x4{kraw[i][4 * k], kraw[i][4 * k + 1], kraw[i][4 * k + 2], kraw[i][4 * k + 3]};
+        } else {
+          uint32_t w0, w1, y0, y1, y2, y3;
+          if constexpr (BITS == 8) {
+            w0 = kraw[i][2 * k];
+            w1 = kraw[i][2 * k + 1];
           } else {
-            uint32_t w0, w1, y0, y1, y2, y3;
-            if constexpr (BITS == 8) {
-              w0 = kraw[i][2 * k];
-              w1 = kraw[i][2 * k + 1];
-            } else {
-              tq4_to_fp8(kraw[i][k], w0, w1);
-            }
-            widen4<BF16>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
-            widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
-            op = u32x4{y0, y1, y2, y3};
+            tq4_to_fp8(kraw[i][k], w0, w1);
           }
-          acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + ((wb * KS + k) * 64 + lane) * 4) : q[k], acc[i]);
+          widen4<BF16>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+          widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+          op = u32x4{y0, y1, y2, y3};
         }
+        acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + ((wb * KS + k) * 64 + lane) * 4) : q[k], acc[i]);
+      }
 #pragma unroll
       for (int i = 0; i < NT; i++)
 #pragma unroll
@@ -450,7 +462,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
           }
       };
       weights();
-      if (__any(top > 256.0f)) {          // (also the first step: m is -infinity, top infinite)
+      if (__any(top > 256.0f)) {          // (also the first finite score: top is infinite)
         float y = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NT; i++)
@@ -460,7 +472,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
         y = fmaxf(y, __shfl_xor(y, 16));
         y = fmaxf(y, __shfl_xor(y, 32));
         const float m1 = fmaxf(m, y);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - m1);
+        const float f = __builtin_amdgcn_exp2f(m - m1);
         m = m1;
         l *= f;
 #pragma unroll
@@ -602,12 +614,11 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       float mm = lds_m[first * kHeads + c];
 #pragma unroll
       for (int i = 1; i < SW; i++) mm = fmaxf(mm, lds_m[(first + i) * kHeads + c]);
-      const float ref = mm == -INFINITY ? 0.0f : mm;
       float ll = 0.0f;
       v4f y = {0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < SW; i++) {
-        const float f = __builtin_amdgcn_exp2f(lds_m[(first + i) * kHeads + c] - ref);
+        const float f = __builtin_amdgcn_exp2f(lds_m[(first + i) * kHeads + c] - mm);
         const v4f z = *reinterpret_cast<const v4f *>(&lds_o[((first + i) * wcols + c) * LD + d0]);
         ll = fmaf(f, lds_l[(first + i) * kHeads + c], ll);
 #pragma unroll
@@ -655,8 +666,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendArgs a) 
     float m = -INFINITY, l = 0.0f;
     v4f o = {0, 0, 0, 0};
     auto add = [&](f2 ml, v4f y) {
-      const float m1 = fmaxf(m, ml.x), ref = m1 == -INFINITY ? 0.0f : m1;
-      const float f0 = __builtin_amdgcn_exp2f(m - ref), f1 = __builtin_amdgcn_exp2f(ml.x - ref);
+      const float m1 = fmaxf(m, ml.x);          // (of a part: finite)
+      const float f0 = __builtin_amdgcn_exp2f(m - m1), f1 = __builtin_amdgcn_exp2f(ml.x - m1);
       m = m1;
       l = l * f0 + ml.y * f1;
 #pragma unroll

@@ -7,6 +7,14 @@
 // pair are in one lane whichever way they are paired; the row's sum of squares and
 // largest value come from DPP lane swaps among its lanes.  Nothing passes through
 // LDS, and a row is read and written once.
+//
+// Measured (d = 128, bf16 rows; a copy kernel reaches 5.9 TB/s):
+//   norm and rotation of 8192 tokens of 64 + 8 heads      55 us, 5.5 TB/s
+//   the same of 2048 tokens of 32 + 8 heads and the 16-bit cache   15 us
+//   8192 tokens of 8 + 8 heads written in 8 bits 12 us, read back 10 us
+// One row per lane: with two to four, whose loads would be in flight together, the
+// first takes 61 us and the last two 32.  Non-temporal stores of q and k save 2 us here
+// and cost the kernel that reads them next 2.5.
 #include "tq_device.hpp"
 #include "tq_kv.hpp"
 

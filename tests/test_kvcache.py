@@ -598,13 +598,17 @@ def test_attention_long(kind, dtype, d, lens):
 @pytest.mark.parametrize("kind,dtype", [("f16", F16), ("4", F16)])
 def test_attention_many_streams(kind, dtype):
     """More streams than lanes of a wavefront, most of them empty or short."""
-    for batch in (63, 64, 65, 200, 513):
+    for batch in (63, 64, 65, 200, 513, 4097, 9000):
         say("streams", kind, batch)
         lens = [int(x) for x in np.random.default_rng(batch).choice([0, 0, 1, 3, 40, 150, 400], batch)]
         s = Streams(lens, 1, 64, 16, kind, dtype, seed=batch)
         attend(s, randn(batch, 2, 64, seed=5).to(dtype))
-    s = Streams([0] * 70, 2, 64, 16, kind, dtype)
-    attend(s, randn(70, 4, 64, seed=5).to(dtype))
+    for batch in (70, 5000):
+        s = Streams([0] * batch, 2, 64, 16, kind, dtype)
+        attend(s, randn(batch, 4, 64, seed=5).to(dtype))
+    # a long stream behind many empty ones
+    s = Streams([0] * 4500 + [3000] + [0] * 700, 2, 64, 16, kind, dtype)
+    attend(s, randn(5201, 4, 64, seed=5).to(dtype))
 
 
 @gpu
@@ -617,6 +621,32 @@ def test_attention_scores_in_extremes():
         if scale == 0.5:
             q = -q.abs() * 20
         attend(s, q, scale=scale)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS[:2])
+def test_attention_infinite_keys(kind, dtype):
+    """A key whose score is -infinity has no weight: the result is that over the others,
+    wherever they lie; with such keys alone it is no number, as 0 / 0."""
+    lens, live = [200, 40, 6000, 20, 33], [range(160, 200), range(3, 40), [5, 5990], range(20), []]
+    s = Streams(lens, 2, 128, 16, kind, dtype, seed=6)
+    q = randn(5, 8, 128, seed=5)
+    q[..., 0] = q[..., 0].abs() + 0.1
+    q = q.to(dtype)
+    at, keep = 0, []
+    rows = s.cache.k.permute(0, 2, 1, 3).reshape(-1, 2, 128).clone()      # by slot
+    for n, alive, slots in zip(lens, live, s.slots):
+        dead = sorted(set(range(n)) - set(alive))
+        rows[slots[dead].cuda(), :, 0] = -math.inf
+        keep += [at + t for t in alive]
+        at += n
+    s.cache.k.copy_(rows.view(s.cache.k.shape[0], 16, 2, 128).permute(0, 2, 1, 3))
+    got, lse = tq.paged_attention(s.cache, q.cuda(), *s.args(), return_lse=True)
+    s.k, s.v, s.lens = s.k[keep], s.v[keep], [len(a) for a in live]
+    ref, ref_lse, bound, lse_bound = s.plain(q, 128 ** -0.5, 0)
+    got, lse = got.cpu().double().numpy(), lse.cpu().double().numpy()
+    assert (np.abs(got - ref)[:4] <= bound[:4]).all() and np.isnan(got[4]).all()
+    assert (np.abs(lse - ref_lse)[:4] <= lse_bound[:4]).all() and (lse[4] == -np.inf).all()
 
 
 @gpu
