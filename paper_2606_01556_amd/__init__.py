@@ -1,4 +1,6 @@
-"""TwinQuant dual-component W4A4 linear layer on AMD MI355X (gfx950).
+"""TwinQuant dual-component W4A4 linear layer on AMD MI355X (gfx950), and what a
+decoder block computes between such layers: head norms and rotation, a paged
+key-value cache and the attention of the newest token (``kvcache``).
 
 Thin Python binding of ``libtq.so`` (C ABI in ``include/tq.h``).  Every step of
 the layer runs in the library's HIP kernels; this module only marshals

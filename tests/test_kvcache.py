@@ -15,7 +15,9 @@ Tolerances (u = half a unit in the last place of the 16-bit type: 2^-11 for fp16
                    and sums of up to 256 terms, one more rounding of the exponent)
 """
 import ctypes
+import importlib
 import math
+import os
 
 import numpy as np
 import pytest
@@ -219,6 +221,15 @@ def test_binding_refuses_host_tensors():
     for bad in (dict(bits=2), dict(head_dim=96), dict(bits=8, dtype=F16), ):
         with pytest.raises(ValueError):
             tq.empty_kv_cache(**{**dict(pages=2, page_size=16, kv_heads=1, head_dim=64, device="cpu"), **bad})
+
+
+def test_missing_binding_raises(monkeypatch):
+    """No fallback: without its built half the binding says what to build."""
+    kv = importlib.import_module("paper_2606_01556_amd.kvcache")
+    monkeypatch.setattr(kv, "_native", None)
+    monkeypatch.setattr(kv, "_HERE", os.path.join(os.path.dirname(kv.__file__), "csrc"))
+    with pytest.raises(RuntimeError, match="_tqtorch.so is missing"):
+        tq.qk_norm_rope(torch.zeros(1, 2, 64, dtype=F16), torch.zeros(1, 1, 64, dtype=F16), None, None)
 
 
 @gpu
