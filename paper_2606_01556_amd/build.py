@@ -45,7 +45,7 @@ def build_binding(verbose: bool = False) -> str:
            *(x for d in (os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
                          sysconfig.get_paths()["include"]) for x in ("-isystem", d)),
            "-I", os.path.join(ROOT, "include"), os.path.join(HERE, "csrc", "tq_torch.cpp"), "-o", BINDING + ".tmp",
-           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_hip", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)

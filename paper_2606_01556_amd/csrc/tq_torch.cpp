@@ -5,6 +5,7 @@
 // entry points of libtq.so, whose addresses the Python side passes in once.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 
 #include <cmath>
 #include <cstdarg>
@@ -87,6 +88,11 @@ void *plain(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef 
 }
 void *plain_or_null(PyObject *o, const char *name, at::ScalarType type, at::IntArrayRef shape, int64_t device) {
   return o == Py_None ? nullptr : plain(o, name, type, shape, device);
+}
+
+// a new tensor's memory from torch's allocator, without the dispatcher's way there
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, int64_t device) {
+  return at::detail::empty_cuda(shape, type, at::Device(at::kCUDA, (at::DeviceIndex)device), std::nullopt);
 }
 
 // rows [tokens, heads, head_dim] (tokens, heads: -1 for any number)
@@ -245,9 +251,9 @@ PyObject *read(PyObject *const *a, Py_ssize_t) {
       fail(PyExc_TypeError, "bf16: the cache holds %s", c.c.dtype == TQ_BF16 ? "bfloat16" : "float16");
     bf16 = c.c.dtype == TQ_BF16;
   }
-  const at::TensorOptions options = at::TensorOptions(at::Device(at::kCUDA, (int8_t)dev)).dtype(bf16 ? at::kBFloat16 : at::kHalf);
-  const at::Tensor k = at::empty({tokens, c.c.kv_heads, c.c.head_dim}, options);
-  const at::Tensor v = at::empty({tokens, c.c.kv_heads, c.c.head_dim}, options);
+  const at::ScalarType type = bf16 ? at::kBFloat16 : at::kHalf;
+  const at::Tensor k = fresh({tokens, c.c.kv_heads, c.c.head_dim}, type, dev);
+  const at::Tensor v = fresh({tokens, c.c.kv_heads, c.c.head_dim}, type, dev);
   if (tokens > 0)
     check(L.read(&c.c, slots, tokens, k.data_ptr(), v.data_ptr(), bf16 ? TQ_BF16 : TQ_F16, to_stream(a[4])), "tq_kv_read");
   return wrap2(k, v);
@@ -291,7 +297,7 @@ PyObject *norm_rope(PyObject *const *a, Py_ssize_t) {
   same_type(kt, "k", type);
   const int hkv = size32(kt.size(1), "k");
   const tq_norm_rope p = norm_rope_args(a + 2, tokens, d, type, dev);
-  const at::Tensor qo = at::empty({tokens, hq, d}, qt.options()), ko = at::empty({tokens, hkv, d}, qt.options());
+  const at::Tensor qo = fresh({tokens, hq, d}, qt.scalar_type(), dev), ko = fresh({tokens, hkv, d}, qt.scalar_type(), dev);
   if (tokens > 0)
     check(L.norm_rope(&p, &q, &k, tokens, hq, hkv, (int)d, dtype_of(type), qo.data_ptr(), ko.data_ptr(), to_stream(a[9])),
           "tq_qk_norm_rope");
@@ -314,9 +320,9 @@ PyObject *norm_rope_append(PyObject *const *a, Py_ssize_t) {
   const int64_t *slots = slots_of(a[4], tokens, dev);
   const tq_norm_rope p = norm_rope_args(a + 5, tokens, d, type, dev);
   const bool return_k = to_bool(a[11]);
-  const at::Tensor qo = at::empty({tokens, hq, d}, qt.options());
+  const at::Tensor qo = fresh({tokens, hq, d}, qt.scalar_type(), dev);
   at::Tensor ko;
-  if (return_k) ko = at::empty({tokens, hkv, d}, qt.options());
+  if (return_k) ko = fresh({tokens, hkv, d}, qt.scalar_type(), dev);
   if (tokens > 0)
     check(L.norm_rope_append(&p, &c.c, &q, &k, &v, slots, tokens, hq, dtype_of(type), qo.data_ptr(),
                              return_k ? ko.data_ptr() : nullptr, to_stream(a[13])),
@@ -350,11 +356,10 @@ PyObject *attend(PyObject *const *a, Py_ssize_t) {
   const int win = window > INT32_MAX ? 0 : (int)window;      // (past any length: none)
   const bool return_lse = to_bool(a[6]);
   const size_t bytes = L.scratch_bytes(&c.c, batch, hq, pages, win);
-  const at::Tensor out = at::empty({batch, hq, d}, qt.options());
-  const at::TensorOptions f32 = qt.options().dtype(at::kFloat);
+  const at::Tensor out = fresh({batch, hq, d}, qt.scalar_type(), dev);
   at::Tensor lse, scratch;
-  if (return_lse) lse = at::empty({batch, hq}, f32);
-  if (bytes > 0) scratch = at::empty({(int64_t)(bytes / 4)}, f32);
+  if (return_lse) lse = fresh({batch, hq}, at::kFloat, dev);
+  if (bytes > 0) scratch = fresh({(int64_t)(bytes / 4)}, at::kFloat, dev);
   if (batch > 0)
     check(L.attend(&c.c, &q, dtype_of(qt.scalar_type()), batch, hq, static_cast<const int32_t *>(pt.data_ptr()), pt.stride(0),
                    pages, lengths, scale, win, out.data_ptr(), return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr,
