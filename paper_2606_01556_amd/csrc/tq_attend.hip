@@ -102,6 +102,16 @@ __device__ __forceinline__ void widen4(uint32_t w, float scale, uint32_t &lo, ui
   }
 }
 
+// Bytes I of w0 and J of w1, codes as tq4_to_fp8 gives them (sign, four zeros, three bits),
+// as the high bytes of two fp16 values: the three bits end below the second exponent
+// bit, where fp16's subnormals and the next binade have the same steps, so the value is
+// the code times 2^-16, exactly, for one instruction.
+constexpr float kSmall = 65536.0f;
+template <int I, int J>
+__device__ __forceinline__ uint32_t small_halves(uint32_t w0, uint32_t w1) {
+  return __builtin_amdgcn_perm(w1, w0, (uint32_t)(4 + J) << 24 | 0x0c0000u | I << 8 | 0x0cu);
+}
+
 // two fp32 values rounded to a word of 16-bit ones
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {
@@ -224,6 +234,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
   constexpr bool VBF = BITS == 16 && BF16;    // type of the second product: bf16, else fp16
   constexpr int LD = D + 4;
   constexpr bool QL = q_in_lds(D, BITS);
+  constexpr bool SK = BITS == 4 && !BF16;     // keys as small_halves
 
   extern __shared__ __attribute__((aligned(16))) float lds[];
   float *const lds_m = lds, *const lds_l = lds + W * kHeads, *const lds_q = lds + 2 * W * kHeads,
@@ -362,7 +373,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     // Q^T: column r, the values of the runs a key lane loads; c1: what a score's
     // product with the key's scale is multiplied by, log2(e) |scale| (its sign goes to Q)
     u32x4 q[KS];
-    const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);     // (-infinity times it has to stay so)
+    const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f) * (SK ? kSmall : 1.0f);     // (-infinity times it has to stay so)
     {
       const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + h0 + min(wb * kHeads + r, a.group - h0 - 1)) * a.q_hs;
       const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, live = r < heads ? 0xffffffffu : 0u;
@@ -401,9 +412,13 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
           } else {
             tq4_to_fp8(kraw[i][k], w0, w1);
           }
-          widen4<BF16>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
-          widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
-          op = u32x4{y0, y1, y2, y3};
+          if constexpr (SK) {
+            op = u32x4{small_halves<0, 1>(w0, w0), small_halves<2, 3>(w0, w0), small_halves<0, 1>(w1, w1), small_halves<2, 3>(w1, w1)};
+          } else {
+            widen4<BF16>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+            widen4<BF16>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+            op = u32x4{y0, y1, y2, y3};
+          }
         }
         acc[i] = mfma16<BF16>(op, QL ? *reinterpret_cast<const u32x4 *>(lds_q + ((wb * KS + k) * 64 + lane) * 4) : q[k], acc[i]);
       }
@@ -531,12 +546,19 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
                   pair[k] = (VBr < 4 ? r & 1 : (c >> 2) & 1) ? hi : lo;
                 }
               }
-              const uint32_t p01 = __builtin_amdgcn_perm(pair[1], pair[0], 0x05010400u);
-              const uint32_t p23 = __builtin_amdgcn_perm(pair[1], pair[0], 0x07030602u);
-              uint32_t w0, w1, w2, w3;
-              widen4<VBF>(p01, BITS == 4 ? 512.0f : 1.0f, w0, w1);
-              widen4<VBF>(p23, BITS == 4 ? 512.0f : 1.0f, w2, w3);
-              op[0][j] = w0; op[1][j] = w1; op[2][j] = w2; op[3][j] = w3;
+              if constexpr (BITS == 4) {
+                op[0][j] = small_halves<0, 0>(pair[0], pair[1]);
+                op[1][j] = small_halves<1, 1>(pair[0], pair[1]);
+                op[2][j] = small_halves<2, 2>(pair[0], pair[1]);
+                op[3][j] = small_halves<3, 3>(pair[0], pair[1]);
+              } else {
+                const uint32_t p01 = __builtin_amdgcn_perm(pair[1], pair[0], 0x05010400u);
+                const uint32_t p23 = __builtin_amdgcn_perm(pair[1], pair[0], 0x07030602u);
+                uint32_t w0, w1, w2, w3;
+                widen4<VBF>(p01, 1.0f, w0, w1);
+                widen4<VBF>(p23, 1.0f, w2, w3);
+                op[0][j] = w0; op[1][j] = w1; op[2][j] = w2; op[3][j] = w3;
+              }
             }
 #pragma unroll
             for (int k = 0; k < 4; k++) {
@@ -597,7 +619,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 #pragma unroll
         for (int c = 0; c < DV; c += 4)
           *reinterpret_cast<v4f *>(&lds_o[(w * wcols + r) * LD + DV * (4 * g + i) + c]) =
-              v4f{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]};
+              v4f{o[c][i], o[c + 1][i], o[c + 2][i], o[c + 3][i]} * (BITS == 4 ? kSmall : 1.0f);
     }
     __syncthreads();
     const bool whole = n == rg.steps;
