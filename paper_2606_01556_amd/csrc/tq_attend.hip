@@ -38,11 +38,11 @@
 //   1 stream of 131072 tokens, 8 kv heads, fp16              88 us, 6.1 TB/s
 //   32 streams up to 8192, bf16                              95 us, 6.1 TB/s
 //   64 streams up to 8192, 8 bits, pages of 64              101 us, 5.8 TB/s
-//   48 streams up to 16384, 4 bits, pages of 16              85 us, 5.2 TB/s
-// of which the first launch keeps the memory busy for 80, 88, 91 and 75 us (6.5 TB/s
-// and more, 4 bits with their scales' 32-byte runs), the ends of the work-groups are 4
-// to 5 apart, and the join takes 4 to 6.  At 4 bits the vector ALU is 55 % busy, at 16
-// bits 9 %.  Without effect or worse: e4m3 products of the keys with Q split into e4m3
+//   48 streams up to 16384, 4 bits, pages of 16              84 us, 5.2 TB/s
+// of which the first launch takes 81, 89, 95 and 78 us (6.2 to 6.6 TB/s of what it reads,
+// at 4 bits 9 % more than it has to: the scales of 16 tokens are 32 bytes), its
+// work-groups ending 4 to 5 us apart, and the join the rest.  At 4 bits the vector ALU
+// is 52 % busy, at 16 bits 9 %.  Without effect or worse: e4m3 products of the keys with Q split into e4m3
 // terms (and scores off by 2^-15 of sum |q k|), eight wavefronts in one work-group, a
 // join by whichever work-group comes last (its fences drop the L2s under the others).
 #include <cfloat>
