@@ -20,11 +20,14 @@
 //    16, DV = d / 16), and pairs the rows up with byte permutes.  The scale of a
 //    quantized row is part of its weight.
 //  * The softmax's reference (and with it the scaling of the weights) only moves
-//    when some weight passes 2^8: most steps have no exchange between lanes and no
+//    when some weight passes 65504: most steps have no exchange between lanes and no
 //    rescaling.  A weight enters the products as two 16-bit terms, its rounded value
 //    and what that leaves (fp16 terms for codes and fp16 rows, bf16 ones for bf16
 //    rows): the matrix cores have the time, and one term alone would put 2^-9 of bf16
-//    into every weight.
+//    into every weight.  It moves so that the largest weight becomes 2^12: fp16's smallest
+//    step, 2^-24, is 2^-36 of that or less, and 2^17 small weights beside a large one
+//    lose 2^-20 in all.  (With the largest weight at 1 they all but vanish from 17 e-folds
+//    below it, where a first token that takes most of the weight leaves them.)
 //
 // The work is cut evenly whatever the lengths: all (stream, head) ranges of steps
 // laid end to end are split into equal runs, two to four work-groups a CU, and a
@@ -83,6 +86,10 @@ constexpr int ranges_of(int group) { return (group + kHeads * head_blocks(group)
 constexpr int range_heads(int group) { return group < kHeads * head_blocks(group) ? group : kHeads * head_blocks(group); }
 
 constexpr float kLog2e = 1.4426950408889634f;
+
+// The largest weight that a step may have (fp16's largest value), and the power of two at
+// which the largest one is put when the reference moves.
+constexpr float kTopWeight = 65504.0f, kHeadroom = 12.0f;
 
 template <bool BF16>
 __device__ __forceinline__ v4f mfma16(u32x4 a, u32x4 b, v4f c) {
@@ -479,7 +486,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
           }
       };
       weights();
-      if (__any(top > 256.0f)) {          // (also the first finite score: top is infinite)
+      if (__any(top > kTopWeight)) {          // (also the first finite score: top is infinite)
         float y = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NT; i++)
@@ -488,7 +495,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
             y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? __builtin_amdgcn_logf(scale_of(vs[i], j)) : 0.0f));
         y = fmaxf(y, __shfl_xor(y, 16));
         y = fmaxf(y, __shfl_xor(y, 32));
-        const float m1 = fmaxf(m, y);
+        const float m1 = fmaxf(m, y - kHeadroom);
         const float f = __builtin_amdgcn_exp2f(m - m1);
         m = m1;
         l *= f;

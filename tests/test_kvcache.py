@@ -635,6 +635,32 @@ def test_attention_scores_in_extremes():
 
 
 @gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("lens", [[60000, 7], [900]])
+def test_attention_small_weights(kind, dtype, lens):
+    """A first token 17.5 e-folds above the rest: in all channels but one the result is
+    that of the many small weights beside it."""
+    say("small weights", kind, dtype, lens)
+    s = Streams(lens, 2, 128, 16, kind, dtype, seed=7)
+    total = sum(lens)
+    k = 0.02 * randn(total, 2, 128, seed=8)
+    v = 1.0 + 0.1 * randn(total, 2, 128, seed=9)
+    at = 0
+    for n in lens:
+        k[at], v[at] = 0.0, 0.0
+        k[at, :, 0], v[at, :, 0] = 14.0, 1.0
+        at += n
+    every = torch.cat(s.slots)
+    tq.kv_append(s.cache, k.to(dtype).cuda(), v.to(dtype).cuda(), every.cuda())
+    (kv, ks), (vv, vs) = stored(s.cache, every)
+    s.k = kv if ks is None else kv * ks.astype(np.float64)[..., None]
+    s.v = vv if vs is None else vv * vs.astype(np.float64)[..., None]
+    q = randn(len(lens), 6, 128, seed=10)
+    q[..., 0] = 20.0                         # 20 * 14 * 0.0625 = 17.5
+    attend(s, q.to(dtype), scale=0.0625)
+
+
+@gpu
 @pytest.mark.parametrize("kind,dtype", KINDS[:2])
 def test_attention_infinite_keys(kind, dtype):
     """A key whose score is -infinity has no weight: the result is that over the others,
