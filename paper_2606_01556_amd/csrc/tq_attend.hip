@@ -62,6 +62,7 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef uint16_t s2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef const int32_t __attribute__((address_space(4))) const_i32;
@@ -465,14 +466,15 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
       float p[NT][4], wt[NT][4], top = 0.0f;
       u32x2 vs[NT];
       if constexpr (BITS < 16) {
-        // (a scale of zero, whose codes are zero, counts as fp16's smallest: p stays bounded)
-        const h2 least = __builtin_bit_cast(h2, 0x00010001u);
+        // (a scale of zero, whose codes are zero, counts as fp16's smallest: p stays bounded.
+        // The larger one by its bits, so that NaN stays.)
+        const s2 least = {1, 1};
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
           for (int k = 0; k < 2; k++) {
             const uint32_t two = k == 0 ? vsr[i].x : vsr[i].y;
-            vs[i][k] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(h2, two), least));
+            vs[i][k] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(s2, two), least));
           }
       }
       auto weights = [&]() {

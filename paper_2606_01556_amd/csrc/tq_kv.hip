@@ -47,12 +47,16 @@ __device__ __forceinline__ float row_sum(float a) {
   if constexpr (L >= 16) a += dpp<0x140>(a);
   return a;
 }
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t a) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, CTRL, 0xF, 0xF, false);
+}
 template <int L>
-__device__ __forceinline__ float row_max(float a) {
-  a = fmaxf(a, dpp<0xB1>(a));
-  a = fmaxf(a, dpp<0x4E>(a));
-  if constexpr (L >= 8) a = fmaxf(a, dpp<0x141>(a));
-  if constexpr (L >= 16) a = fmaxf(a, dpp<0x140>(a));
+__device__ __forceinline__ uint32_t row_max(uint32_t a) {
+  a = max(a, dpp<0xB1>(a));
+  a = max(a, dpp<0x4E>(a));
+  if constexpr (L >= 8) a = max(a, dpp<0x141>(a));
+  if constexpr (L >= 16) a = max(a, dpp<0x140>(a));
   return a;
 }
 
@@ -219,12 +223,15 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
       // the codes of the rounded values
       widen<BF16>(o0, v);
       widen<BF16>(o1, v + 8);
-      float amax = 0.0f;
+      // the largest value by its bits, in which NaN comes after infinity
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 16; i++) amax = fmaxf(amax, fabsf(v[i]));
-      amax = row_max<L>(amax);
-      // (a bf16 row beyond fp16's largest scale saturates)
-      const uint16_t s16 = float_to_half_bits(fminf(amax / (BITS == 4 ? 7.0f : 448.0f), 65504.0f));
+      for (int i = 0; i < 16; i++) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+      top = row_max<L>(top);
+      const float amax = __builtin_bit_cast(float, top);
+      // (a bf16 row beyond fp16's largest scale saturates; one that is not finite gets the
+      // scale NaN, since its codes could not tell)
+      const uint16_t s16 = top >= 0x7f800000u ? 0x7e00 : float_to_half_bits(fminf(amax / (BITS == 4 ? 7.0f : 448.0f), 65504.0f));
       const float s = half_bits_to_float(s16);
       const float y = s == 0.0f ? 0.0f : 1.0f / s;
       if (at < 0) return;

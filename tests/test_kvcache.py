@@ -424,6 +424,35 @@ def test_quantizer_ties(kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["8", "4"])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_not_finite(kind, dtype, d):
+    """A row with an infinity or NaN anywhere reads as NaN, its neighbours as they were
+    without it, and an attention that sees it is NaN, through the key or the value."""
+    rows, heads, bad = 32, 2, {3: math.inf, 9: -math.inf, 17: math.nan, 30: math.nan}
+    k, v = randn(rows, heads, d, seed=1).to(dtype), randn(rows, heads, d, seed=2).to(dtype)
+    for side in (0, 1):
+        c, clean = (make_cache(3, 16, heads, d, kind) for _ in range(2))
+        x = [k.clone(), v.clone()]
+        for i, (r, b) in enumerate(bad.items()):
+            x[side][r, 1, (i * 37 + 5) % d] = b
+        slots = torch.arange(rows).cuda()
+        tq.kv_append(c, x[0].cuda(), x[1].cuda(), slots)
+        tq.kv_append(clean, k.cuda(), v.cuda(), slots)
+        dead = torch.zeros(rows, heads, dtype=torch.bool)
+        dead[list(bad), 1] = True
+        for s, (got, want) in enumerate(zip(tq.kv_read(c, slots), tq.kv_read(clean, slots))):
+            got, want = got.cpu(), want.cpu()
+            hit = dead if s == side else torch.zeros_like(dead)
+            assert got[hit].isnan().all() and torch.equal(got[~hit], want[~hit])
+        q = randn(2, 4, d, seed=3).to(dtype).cuda()
+        table = torch.tensor([[0, 1], [1, 0]], dtype=torch.int32).cuda()
+        out = tq.paged_attention(c, q, table, torch.tensor([3, 16], dtype=torch.int32).cuda())
+        assert out[0].isfinite().all() and out[1, :2].isfinite().all() and out[1, 2:].isnan().all()
+
+
+@gpu
 @pytest.mark.parametrize("kind", ["f16", "8", "4"])
 def test_slots_outside(kind):
     """Slots before and past the cache are neither written nor read."""
