@@ -355,7 +355,8 @@ typedef struct {
  * head_dim] normed and rotated, one launch.
  *   q_out, k_out  of the same shapes, contiguous; either may be the input itself
  *                 where that is contiguous (a row is read before it is written)
- * tokens == 0 is a no-op; tokens * (q_heads + kv_heads) < 2^31.
+ * tokens == 0 is a no-op; rows = tokens * (q_heads + kv_heads) < 2^31, and rows *
+ * head_dim <= 2^36 - 4096.
  * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_HIP. */
 tq_status tq_qk_norm_rope(const tq_norm_rope *p, const tq_head_rows *q, const tq_head_rows *k, int tokens,
                           int q_heads, int kv_heads, int head_dim, tq_dtype dtype, void *q_out, void *k_out,
@@ -365,8 +366,8 @@ tq_status tq_qk_norm_rope(const tq_norm_rope *p, const tq_head_rows *q, const tq
  *   slots  [tokens] int64; a token whose slot is negative or past the cache is not
  *          written; slots of one call are distinct (a slot given twice holds
  *          either token's row)
- * With 16 bits dtype is the cache's.  tokens == 0 is a no-op; 2 * tokens *
- * kv_heads < 2^31.  Errors as above, TQ_ERR_BUFFER for a cache with unsupported
+ * With 16 bits dtype is the cache's.  tokens == 0 is a no-op; limits as above for
+ * rows = 2 * tokens * kv_heads.  Errors as above, TQ_ERR_BUFFER for a cache with unsupported
  * sizes. */
 tq_status tq_kv_append(const tq_kv_cache *c, const tq_head_rows *k, const tq_head_rows *v,
                        const int64_t *slots, int tokens, tq_dtype dtype, void *stream);

@@ -771,7 +771,8 @@ AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int
   //    8 bits  768: 8.3, 8.3  1024:  9.7, 8.3    2048: 20.3, 22.4
   //    4 bits 1024: 8.1, 8.0  1536: 10.2, 8.3    2048: 13.1, 18.6
   const int rounds2 = 32768 / (c.d * c.bits), most_steps = (rounds2 < 32 ? rounds2 : 32) * (ranges >= kCus / 2 ? 2 : 1);
-  p.direct = steps <= most_steps && ranges < ((int64_t)1 << 31);
+  // (and a launch numbers its lanes in 32 bits)
+  p.direct = steps <= most_steps && ranges * 64 * kDirectWaves < ((int64_t)1 << 32);
   p.steps = ranges * steps;
   if (p.direct) {
     p.blocks = (int)ranges;

@@ -68,8 +68,12 @@ tq_status check_norm_rope(const tq_norm_rope *p, int head_dim, tq::TokenArgs &a)
   return TQ_OK;
 }
 
-// the kernels number the rows of a call in 31 bits
-inline bool rows_ok(int tokens, int64_t per_token) { return (int64_t)tokens * per_token < ((int64_t)1 << 31); }
+// The kernels number the rows of a call in 31 bits, and a launch its lanes (16 values
+// each, in work-groups of 256) in 32.
+inline bool rows_ok(int tokens, int64_t per_token, int d) {
+  const int64_t rows = (int64_t)tokens * per_token;
+  return rows < ((int64_t)1 << 31) && rows * (d / 16) <= ((int64_t)1 << 32) - 256;
+}
 
 tq_status hip_status(hipError_t e) { return e == hipSuccess ? TQ_OK : TQ_ERR_HIP; }
 
@@ -91,7 +95,7 @@ tq_status tq_qk_norm_rope(const tq_norm_rope *p, const tq_head_rows *q, const tq
   TQ_TRY(check_rows(q, a.q));
   TQ_TRY(check_rows(k, a.k));
   if (!head_dim_ok(head_dim) || tokens < 0 || q_heads < 1 || kv_heads < 1 || q_heads > 65535 || kv_heads > 1024 ||
-      !rows_ok(tokens, (int64_t)q_heads + kv_heads))
+      !rows_ok(tokens, (int64_t)q_heads + kv_heads, head_dim))
     return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype)) return TQ_ERR_DTYPE;
   TQ_TRY(check_norm_rope(p, head_dim, a));
@@ -112,7 +116,7 @@ tq_status tq_kv_append(const tq_kv_cache *c, const tq_head_rows *k, const tq_hea
   TQ_TRY(check_cache(c, a.c));
   TQ_TRY(check_rows(k, a.k));
   TQ_TRY(check_rows(v, a.v));
-  if (tokens < 0 || !rows_ok(tokens, 2 * (int64_t)c->kv_heads)) return TQ_ERR_SHAPE;
+  if (tokens < 0 || !rows_ok(tokens, 2 * (int64_t)c->kv_heads, c->head_dim)) return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
   if (!aligned(slots, 8)) return TQ_ERR_ALIGN;
   if (tokens == 0) return TQ_OK;
@@ -132,7 +136,7 @@ tq_status tq_qk_norm_rope_append(const tq_norm_rope *p, const tq_kv_cache *c, co
   TQ_TRY(check_rows(q, a.q));
   TQ_TRY(check_rows(k, a.k));
   TQ_TRY(check_rows(v, a.v));
-  if (tokens < 0 || q_heads < 1 || q_heads > 65535 || !rows_ok(tokens, q_heads + 2 * (int64_t)c->kv_heads))
+  if (tokens < 0 || q_heads < 1 || q_heads > 65535 || !rows_ok(tokens, q_heads + 2 * (int64_t)c->kv_heads, c->head_dim))
     return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
   TQ_TRY(check_norm_rope(p, c->head_dim, a));
@@ -151,7 +155,7 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
   tq::ReadArgs a = {};
   if (slots == nullptr || k_out == nullptr || v_out == nullptr) return TQ_ERR_NULL;
   TQ_TRY(check_cache(c, a.c));
-  if (tokens < 0 || !rows_ok(tokens, 2 * (int64_t)c->kv_heads)) return TQ_ERR_SHAPE;
+  if (tokens < 0 || !rows_ok(tokens, 2 * (int64_t)c->kv_heads, c->head_dim)) return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
   if (!aligned(slots, 8) || !aligned16(k_out) || !aligned16(v_out)) return TQ_ERR_ALIGN;
   if (tokens == 0) return TQ_OK;

@@ -207,6 +207,22 @@ def test_attention_validation():
     assert size(desc(), 9, 4, 4, 0) == 0 and size(desc(), 9, 4, 400, 100) == 0
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_calls_beyond_a_launch(d):
+    """A launch holds 2^32 lanes: calls of more rows are refused before it, attentions of
+    more ranges run in fewer work-groups than ranges."""
+    L, c = tq.lib(), desc(kv_heads=1024, head_dim=d)
+    rows = (1 << 36) // d                       # one more than fit
+    row = tq.kvcache._HeadRows(FAKE, 0, 0)
+    assert L.tq_kv_append(c, row, row, FAKE, rows // 2048, 0, None) == 2
+    assert L.tq_kv_read(c, FAKE, rows // 2048, FAKE, FAKE, 0, None) == 2
+    p = rope(rotary_dim=0, positions=None, table=None)
+    assert L.tq_qk_norm_rope(p, row, row, rows // 2048, 1024, 1024, d, 0, FAKE, FAKE, None) == 2
+    assert L.tq_qk_norm_rope_append(p, c, row, row, row, FAKE, rows // 4096, 2048, 0, FAKE, None, None) == 2
+    size = lambda batch: L.tq_paged_attention_scratch_bytes(c, batch, 1024, 1, 0)
+    assert size(8191) == 0 < size(8192)
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros(2, 4, 128, dtype=F16)
     with pytest.raises(ValueError):
