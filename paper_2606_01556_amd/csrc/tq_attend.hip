@@ -91,6 +91,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The largest weight that a step may have (fp16's largest value), and the power of two at
 // which the largest one is put when the reference moves.
 constexpr float kTopWeight = 65504.0f, kHeadroom = 12.0f;
+constexpr float kLeastScale = 0x1p-24f;    // fp16's smallest number
 
 template <bool BF16>
 __device__ __forceinline__ v4f mfma16(u32x4 a, u32x4 b, v4f c) {
@@ -463,7 +464,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     };
     // weights p in s, times the values' scales
     auto softmax = [&]() {
-      float p[NT][4], wt[NT][4], top = 0.0f;
+      float p[NT][4], wt[NT][4], top = 0.0f, ptop = 0.0f;
       u32x2 vs[NT];
       if constexpr (BITS < 16) {
         // (a scale of zero, whose codes are zero, counts as fp16's smallest: p stays bounded.
@@ -485,7 +486,11 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
             p[i][j] = __builtin_amdgcn_exp2f(fmaf(s[i][j], c1, -m));
             wt[i][j] = BITS < 16 ? fmaf(p[i][j], scale_of(vs[i], j), 0.0f) : p[i][j];
             top = fmaxf(top, wt[i][j]);
+            if constexpr (BITS < 16) ptop = fmaxf(ptop, p[i][j]);
           }
+        // (a scale that is NaN counts as fp16's smallest, so that the sum of p stays one; the
+        // others leave top as it is)
+        if constexpr (BITS < 16) top = fmaxf(top, ptop * kLeastScale);
       };
       weights();
       if (__any(top > kTopWeight)) {          // (also the first finite score: top is infinite)
@@ -494,7 +499,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
         for (int i = 0; i < NT; i++)
 #pragma unroll
           for (int j = 0; j < 4; j++)
-            y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? __builtin_amdgcn_logf(scale_of(vs[i], j)) : 0.0f));
+            y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? fmaxf(__builtin_amdgcn_logf(scale_of(vs[i], j)), -24.0f) : 0.0f));
         y = fmaxf(y, __shfl_xor(y, 16));
         y = fmaxf(y, __shfl_xor(y, 32));
         const float m1 = fmaxf(m, y - kHeadroom);

@@ -1,0 +1,66 @@
+"""The operators between the linear layers at the ends of their types: values near
+bf16's largest and far below one, weights whose low bits decide, rows past the
+largest scale, infinities and NaN in live rows.
+
+Tolerances: as in test_attention_plans, with
+  2^-20   of sum_t w_t |v_t| where the scores are at most 8 and their own sums are of
+          two products: such a score is off by 2^-22, its exponent, of at most 16
+          binades, by 2^-21 (0.7 of that in the weight), exp2 by 2^-23; a weight of
+          16 bits would be off by up to 2^-18"""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2606_01556_amd as tq
+from test_attention_plans import Held
+from test_kvcache import BF16, F16, KINDS, make_cache, randn, say, stored, ulp
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _wait():
+    yield
+    torch.cuda.synchronize()
+
+
+def refill(s, k, v, dtype):
+    """The streams' rows replaced by k and v [all tokens, heads, d]."""
+    every = torch.cat(s.slots)
+    tq.kv_append(s.cache, k.to(dtype).cuda(), v.to(dtype).cuda(), every.cuda())
+    (kv, ks), (vv, vs) = stored(s.cache, every)
+    s.k = kv if ks is None else kv * ks.astype(np.float64)[..., None]
+    s.v = vv if vs is None else vv * vs.astype(np.float64)[..., None]
+
+
+def run(s, q, **kw):
+    out, lse = tq.paged_attention(s.cache, q.cuda(), *s.args(), return_lse=True, **kw)
+    return out.cpu().double().numpy(), lse.cpu().double().numpy()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("kind,dtype", KINDS[2:])
+def test_sum_with_values_that_are_no_number(kind, dtype, d):
+    """The log-sum-exp is the keys' alone: value rows whose scale is NaN, all or one of
+    them, far above the others or not, leave it as it is."""
+    lens = [1, 40, 3000, 60, 3001, 700, 33]
+    s = Held(lens, 2, d, 16, kind, dtype, seed=d)
+    k, v = randn(sum(lens), 2, d, seed=1), randn(sum(lens), 2, d, seed=2)
+    at = np.cumsum([0] + lens)
+    v[at[0]:at[3], :, 5] = math.nan               # all rows of the first three streams
+    for i in (3, 4, 5):                           # one row of the others but the last
+        row = at[i] + lens[i] // 2
+        v[row, :, 9] = math.nan
+        if i < 5:
+            k[row, :, 0] = 40.0
+    refill(s, k, v, dtype)
+    q = randn(len(lens), 6, d, seed=3)
+    q[..., 0] = 40.0                              # 40 * 40 / d^0.5: 100 and more e-folds above the others
+    q = q.to(dtype)
+    got, lse = run(s, q)
+    with np.errstate(invalid="ignore"):
+        ref, ref_lse, bound, lse_bound = s.plain(q, d ** -0.5, 0)
+    assert (np.abs(lse - ref_lse) <= lse_bound).all()
+    assert np.isnan(got[:6]).all() and (np.abs(got[6] - ref[6]) <= bound[6]).all()
