@@ -20,14 +20,16 @@
 //    16, DV = d / 16), and pairs the rows up with byte permutes.  The scale of a
 //    quantized row is part of its weight.
 //  * The softmax's reference (and with it the scaling of the weights) only moves
-//    when some weight passes 65504: most steps have no exchange between lanes and no
+//    when some weight passes 65504 (bf16 rows: 1 over the number of tokens): most steps have no exchange between lanes and no
 //    rescaling.  A weight enters the products as two 16-bit terms, its rounded value
 //    and what that leaves (fp16 terms for codes and fp16 rows, bf16 ones for bf16
 //    rows): the matrix cores have the time, and one term alone would put 2^-9 of bf16
 //    into every weight.  It moves so that the largest weight becomes 2^12: fp16's smallest
 //    step, 2^-24, is 2^-36 of that or less, and 2^17 small weights beside a large one
 //    lose 2^-20 in all.  (With the largest weight at 1 they all but vanish from 17 e-folds
-//    below it, where a first token that takes most of the weight leaves them.)
+//    below it, where a first token that takes most of the weight leaves them.)  With bf16
+//    rows it becomes 2^-8 over the number of tokens, or less: bf16 terms have fp32's exponents,
+//    and a sum of values near bf16's largest must not pass fp32's.
 //
 // The work is cut evenly whatever the lengths: all (stream, head) ranges of steps
 // laid end to end are split into equal runs, two to four work-groups a CU, and a
@@ -91,6 +93,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The largest weight that a step may have (fp16's largest value), and the power of two at
 // which the largest one is put when the reference moves.
 constexpr float kTopWeight = 65504.0f, kHeadroom = 12.0f;
+// With bf16 rows, whose values fp32 itself just holds, the weights of a range of fewer than
+// 2^e tokens stay at 2^-e or below, so that no sum passes the largest value; the largest
+// weight is put kBelow binades lower.
+constexpr int kBelow = 8;
 constexpr float kLeastScale = 0x1p-24f;    // fp16's smallest number
 
 template <bool BF16>
@@ -212,8 +218,10 @@ constexpr int lds_floats(int waves, int hb, int d, int bits, int cols) {
 template <bool BF16>
 __device__ __forceinline__ void store4(const AttendArgs &a, int d, int64_t row, int d0, float m, float l, v4f o) {
   const float inv = 1.0f / l;
+  int e;
+  const float f = frexpf(l, &e);         // (m and l's binade all but cancel: they go together first)
   *reinterpret_cast<u32x2 *>(a.out + row * d + d0) = u32x2{pack2<BF16>(o[0] * inv, o[1] * inv), pack2<BF16>(o[2] * inv, o[3] * inv)};
-  if (a.lse != nullptr && d0 == 0) a.lse[row] = (m + log2f(l)) * (1.0f / kLog2e);
+  if (a.lse != nullptr && d0 == 0) a.lse[row] = (m + (float)e + log2f(f)) * (1.0f / kLog2e);
 }
 
 // What the first launch tells the join about a range, [batch][vheads]: the number
@@ -404,6 +412,12 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     // (finite, so that keys whose score is -infinity have the weight 0 also before the
     // first finite one)
     float m = -FLT_MAX, l = 0.0f;
+    float most = kTopWeight, headroom = kHeadroom;
+    if constexpr (VBF) {
+      const int e = 32 - __builtin_clz(rg.len);
+      most = __builtin_bit_cast(float, (127 - e) << 23);
+      headroom = (float)(-e - kBelow);
+    }
     float s[NT][4];
     // scores, times the keys' scales: row 4 g + j of tile i, head r
     auto scores = [&]() {
@@ -493,7 +507,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
         if constexpr (BITS < 16) top = fmaxf(top, ptop * kLeastScale);
       };
       weights();
-      if (__any(top > kTopWeight)) {          // (also the first finite score: top is infinite)
+      if (__any(top > most)) {                // (also the first finite score: top is infinite)
         float y = -INFINITY;
 #pragma unroll
         for (int i = 0; i < NT; i++)
@@ -502,7 +516,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
             y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? fmaxf(__builtin_amdgcn_logf(scale_of(vs[i], j)), -24.0f) : 0.0f));
         y = fmaxf(y, __shfl_xor(y, 16));
         y = fmaxf(y, __shfl_xor(y, 32));
-        const float m1 = fmaxf(m, y - kHeadroom);
+        const float m1 = fmaxf(m, y - headroom);
         const float f = __builtin_amdgcn_exp2f(m - m1);
         m = m1;
         l *= f;

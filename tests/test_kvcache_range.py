@@ -64,3 +64,26 @@ def test_sum_with_values_that_are_no_number(kind, dtype, d):
         ref, ref_lse, bound, lse_bound = s.plain(q, d ** -0.5, 0)
     assert (np.abs(lse - ref_lse) <= lse_bound).all()
     assert np.isnan(got[:6]).all() and (np.abs(got[6] - ref[6]) <= bound[6]).all()
+
+
+@pytest.mark.parametrize("d,lens", [(64, [1, 40, 0, 5000]), (128, [300, 17, 9000]), (256, [200, 3]), (256, [4100, 64]), (64, [70000])])
+@pytest.mark.parametrize("exponent", [127, 120, 0, -60, -90])
+def test_bf16_values_of_any_size(exponent, d, lens):
+    """Values up to bf16's largest, and far below one: the result is as good as at one."""
+    say("values of 2^", exponent, d, lens)
+    s = Held(lens, 2, d, 16, "bf16", BF16, seed=d)
+    v = randn(sum(lens), 2, d, seed=2).clamp(-1.9, 1.9).double()
+    v[:, :, 3] = 1.9921875                        # times 2^127: the largest value there is
+    v[:, :, 4] = -v[:, :, 3]
+    refill(s, randn(sum(lens), 2, d, seed=1), v * 2.0 ** exponent, BF16)
+    s.v = s.v * 2.0 ** -exponent
+    for scale in (None, 0.0):                     # (0: all weights alike)
+        q = randn(len(lens), 8, d, seed=3).to(BF16)
+        got, lse = run(s, q, scale=scale)
+        ref, ref_lse, bound, lse_bound = s.plain(q, d ** -0.5 if scale is None else scale, 0)
+        live = np.isfinite(ref_lse)
+        bound[live] += 2.0 ** (-133 - exponent) - 2.0 ** -24     # (no floor but the type's own smallest step)
+        assert np.isfinite(got).all()
+        over = (np.abs(got * 2.0 ** -exponent - ref) - bound).max()
+        assert over <= 0, over
+        assert (np.abs(lse - ref_lse)[live] <= lse_bound[live]).all() and np.isinf(lse[~live]).all()
