@@ -405,8 +405,9 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
  *               aligned, free again when the stream has run the call; may be NULL
  *               where that size is 0 (short streams)
  * What slots outside a stream's range hold (NaN too) has no effect.  Scores, the
- * softmax and the sums are fp32; the softmax's weights enter the products with v
- * with 16 bits or more, or to 2^-37 of the largest weight.  One launch for short streams, else two; the result does not
+ * softmax and the sums are fp32; the softmax's weights enter the products with v with
+ * all their bits (16-bit cache of bf16 values) or with 22, or to 2^-37 of the largest
+ * weight (else).  One launch for short streams, else two; the result does not
  * depend on timing.  batch == 0 is a no-op; batch <= 65535, max_pages
  * * page_size <= 2^30, q_heads a multiple of kv_heads, at most 65535; all streams' and
  * heads' tokens, as the page table bounds them, in units of 32 below 2^31 - 2^16.

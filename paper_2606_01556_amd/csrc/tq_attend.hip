@@ -20,16 +20,19 @@
 //    16, DV = d / 16), and pairs the rows up with byte permutes.  The scale of a
 //    quantized row is part of its weight.
 //  * The softmax's reference (and with it the scaling of the weights) only moves
-//    when some weight passes 65504 (bf16 rows: 1 over the number of tokens): most steps have no exchange between lanes and no
-//    rescaling.  A weight enters the products as two 16-bit terms, its rounded value
-//    and what that leaves (fp16 terms for codes and fp16 rows, bf16 ones for bf16
-//    rows): the matrix cores have the time, and one term alone would put 2^-9 of bf16
-//    into every weight.  It moves so that the largest weight becomes 2^12: fp16's smallest
-//    step, 2^-24, is 2^-36 of that or less, and 2^17 small weights beside a large one
-//    lose 2^-20 in all.  (With the largest weight at 1 they all but vanish from 17 e-folds
-//    below it, where a first token that takes most of the weight leaves them.)  With bf16
-//    rows it becomes 2^-8 over the number of tokens, or less: bf16 terms have fp32's exponents,
-//    and a sum of values near bf16's largest must not pass fp32's.
+//    when some weight passes 65504 (bf16 rows: 1 over the number of tokens): most
+//    steps have no exchange between lanes and no rescaling.
+//  * A weight enters the products as several 16-bit terms, as the matrix cores have
+//    the time: for codes and fp16 rows two fp16 ones, its rounded value and what that
+//    leaves (22 bits); for bf16 rows three bf16 ones, which hold all 24 (two of them
+//    left 2^-18 of every weight; the third costs up to 1 %: 95 us for 32 streams up to
+//    8192 either way, 65.4 after 64.9 for 16 of 4096 at d = 256).
+//  * With fp16 terms the reference moves so that the largest weight becomes 2^12:
+//    fp16's smallest step, 2^-24, is 2^-36 of that or less, and 2^17 small weights
+//    beside a large one lose 2^-20 in all.  (With the largest weight at 1 they all but
+//    vanish from 17 e-folds below it, where a first token that takes most of the weight
+//    leaves them.)  With bf16 ones, which have fp32's exponents, it becomes 2^-8 over the
+//    number of tokens, or less: a sum of values near bf16's largest must not pass fp32's.
 //
 // The work is cut evenly whatever the lengths: all (stream, head) ranges of steps
 // laid end to end are split into equal runs, two to four work-groups a CU, and a
@@ -136,12 +139,8 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
   if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
   else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
 }
-// the two values of such a word
-template <bool BF16>
-__device__ __forceinline__ f2 unpack2(uint32_t w) {
-  if constexpr (BF16) return f2{__builtin_bit_cast(float, w << 16), __builtin_bit_cast(float, w & 0xffff0000u)};
-  else return __builtin_convertvector(__builtin_bit_cast(h2, w), f2);
-}
+// the two values of a word of fp16 ones
+__device__ __forceinline__ f2 unpack2(uint32_t w) { return __builtin_convertvector(__builtin_bit_cast(h2, w), f2); }
 
 // NB bytes from p (p aligned to min(NB, 16)).  The cache is read once per call:
 // non-temporal loads stream it at 7.0 TB/s instead of 6.2 (512 MB).
@@ -251,6 +250,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
   constexpr uint32_t VB = VBr < 4 ? 4 : VBr;
   constexpr int VW = (int)VB / 4;
   constexpr bool VBF = BITS == 16 && BF16;    // type of the second product: bf16, else fp16
+  constexpr int TERMS = VBF ? 3 : 2;          // of a weight
   constexpr int LD = D + 4;
   constexpr bool QL = q_in_lds(D, BITS);
   constexpr bool SK = BITS == 4 && !BF16;     // keys as small_halves
@@ -536,13 +536,25 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     auto products = [&]() {
 #pragma unroll
       for (int i = 0; i < NT; i += 2) {
-        u32x4 ph, pl;
+        u32x4 pt[TERMS];
 #pragma unroll
         for (int j = 0; j < 4; j++) {
           const int h = i + j / 2, k = 2 * (j & 1);
-          ph[j] = pack2<VBF>(s[h][k], s[h][k + 1]);
-          const f2 u = unpack2<VBF>(ph[j]);
-          pl[j] = pack2<VBF>(fmaf(u.x, -1.0f, s[h][k]), fmaf(u.y, -1.0f, s[h][k + 1]));
+          if constexpr (VBF) {
+            // the upper halves, three times over: all 24 bits
+            float x = s[h][k], y = s[h][k + 1];
+#pragma unroll
+            for (int t = 0; t < TERMS; t++) {
+              const uint32_t xb = __builtin_bit_cast(uint32_t, x), yb = __builtin_bit_cast(uint32_t, y);
+              pt[t][j] = __builtin_amdgcn_perm(yb, xb, 0x07060302u);
+              x -= __builtin_bit_cast(float, xb & 0xffff0000u);
+              y -= __builtin_bit_cast(float, yb & 0xffff0000u);
+            }
+          } else {
+            pt[0][j] = pack2<false>(s[h][k], s[h][k + 1]);
+            const f2 u = unpack2(pt[0][j]);
+            pt[1][j] = pack2<false>(fmaf(u.x, -1.0f, s[h][k]), fmaf(u.y, -1.0f, s[h][k + 1]));
+          }
         }
         if constexpr (BITS == 16) {
           // two channels a word: rows 2 j and 2 j + 1 paired up
@@ -553,8 +565,8 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 #pragma unroll
             for (int j = 0; j < 4; j++)
               op[j] = __builtin_amdgcn_perm(vraw[i + j / 2][2 * (j & 1) + 1][c / 2], vraw[i + j / 2][2 * (j & 1)][c / 2], sel);
-            o[c] = mfma16<VBF>(op, ph, o[c]);
-            o[c] = mfma16<VBF>(op, pl, o[c]);
+#pragma unroll
+            for (int t = 0; t < TERMS; t++) o[c] = mfma16<VBF>(op, pt[t], o[c]);
           }
         } else {
           // four channels a word of bytes: the bytes paired up, then widened
@@ -591,10 +603,9 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
               }
             }
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-              o[c + k] = mfma16<VBF>(op[k], ph, o[c + k]);
-              o[c + k] = mfma16<VBF>(op[k], pl, o[c + k]);
-            }
+            for (int k = 0; k < 4; k++)
+#pragma unroll
+              for (int t = 0; t < TERMS; t++) o[c + k] = mfma16<VBF>(op[k], pt[t], o[c + k]);
           }
         }
       }

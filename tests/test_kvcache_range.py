@@ -87,3 +87,33 @@ def test_bf16_values_of_any_size(exponent, d, lens):
         over = (np.abs(got * 2.0 ** -exponent - ref) - bound).max()
         assert over <= 0, over
         assert (np.abs(lse - ref_lse)[live] <= lse_bound[live]).all() and np.isinf(lse[~live]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_weights_keep_fp32s_bits(kind, dtype, d):
+    """Two keys of all but one score, values 1 and -1, beside a larger one of value 0: the
+    result is what the two weights differ by."""
+    batch, heads, gen = 256, 2, torch.Generator().manual_seed(1)
+    s = Held([3] * batch, heads, d, 16, kind, dtype, seed=d)
+    k, v = torch.zeros(3 * batch, heads, d), torch.zeros(3 * batch, heads, d)
+    k[:, :, 0] = torch.rand(3 * batch, heads, generator=gen)
+    k[..., 1] = 1.0
+    k[0::3, :, 1] = 1.2
+    v[1::3], v[2::3] = 1.0, -1.0
+    refill(s, k, v, dtype)
+    q = torch.zeros(batch, 8, d)
+    q[..., 0] = 2.0 ** -11
+    q[..., 1] = 4.0 * torch.rand(batch, 8, generator=gen)
+    q = q.to(dtype)
+    got, _ = run(s, q, scale=1.0)
+    for i in range(batch):
+        kk, vv, qq = s.k[3 * i:3 * i + 3], s.v[3 * i:3 * i + 3], q[i].double().numpy()
+        for h in range(8):
+            x = kk[:, h // 4] @ qq[h]
+            w = np.exp(x - x.max())
+            w /= w.sum()
+            o = w @ vv[:, h // 4]
+            bound = ulp(dtype) * np.abs(o) + 2.0 ** -20 * (w @ np.abs(vv[:, h // 4])) + 2.0 ** -24
+            over = (np.abs(got[i, h] - o) - bound).max()
+            assert over <= 0, (i, h, over)
