@@ -315,8 +315,9 @@ tq_status tq_act_codes_canonical(const void *x_codes, const void *x_scales, int 
  * The quantizer is that of Sec. 2 Eq. (1) with the row as its group: scale =
  * fp16(max|x| / 7) and code = clamp(rint(x / scale), -7, 7) at 4 bits, fp16(max|x|
  * / 448) and x / scale rounded half to even to e4m3 at 8; a row whose scale is
- * zero has zero codes.  A row that holds an infinity or NaN has the scale NaN at
- * either width, and so reads as NaN.
+ * zero has zero codes.  A row that holds an infinity or NaN, or whose scale rounds past
+ * fp16's largest number (bf16 values from 458640 on at 4 bits, from 29352960 on at 8), has
+ * the scale NaN, and so reads as NaN.
  * head_dim 64, 128 or 256; page_size a power of two from 16 to 32768; pages *
  * page_size <= 2^40, kv_heads <= 1024. */
 typedef struct {

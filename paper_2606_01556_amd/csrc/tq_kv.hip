@@ -229,9 +229,9 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
       for (int i = 0; i < 16; i++) top = max(top, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
       top = row_max<L>(top);
       const float amax = __builtin_bit_cast(float, top);
-      // (a bf16 row beyond fp16's largest scale saturates; one that is not finite gets the
+      // (a row that is not finite, or a bf16 one whose scale no fp16 number holds, gets the
       // scale NaN, since its codes could not tell)
-      const uint16_t s16 = top >= 0x7f800000u ? 0x7e00 : float_to_half_bits(fminf(amax / (BITS == 4 ? 7.0f : 448.0f), 65504.0f));
+      const uint16_t h = float_to_half_bits(amax / (BITS == 4 ? 7.0f : 448.0f)), s16 = h >= 0x7c00 ? 0x7e00 : h;
       const float s = half_bits_to_float(s16);
       const float y = s == 0.0f ? 0.0f : 1.0f / s;
       if (at < 0) return;

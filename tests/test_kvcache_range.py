@@ -117,3 +117,29 @@ def test_weights_keep_fp32s_bits(kind, dtype, d):
             bound = ulp(dtype) * np.abs(o) + 2.0 ** -20 * (w @ np.abs(vv[:, h // 4])) + 2.0 ** -24
             over = (np.abs(got[i, h] - o) - bound).max()
             assert over <= 0, (i, h, over)
+
+
+@pytest.mark.parametrize("kind,top", [("4", 7), ("8", 448)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_rows_past_the_largest_scale(kind, top, d):
+    """bf16 rows whose scale, max|x| / top, no fp16 number holds have the scale NaN, as
+    rows that are not finite; the largest ones below keep theirs."""
+    c = make_cache(2, 16, 2, d, kind)
+    x = randn(6, 2, d, seed=d).to(BF16)
+    x[1, 0, 7] = top * 65536.0                    # / top: 65536, which rounds to infinity
+    x[2, 1, d - 1] = -top * 65536.0
+    x[3, 0, 0] = 3.3e38
+    x[4, 0, 11] = top * 65536.0 * 0.995           # the next bf16 number below the first: 65280 or less
+    assert float(x[4, 0, 11]) / top < 65504 and float(x[1, 0, 7]) / top == 65536
+    slots = torch.arange(6).cuda()
+    tq.kv_append(c, x.cuda(), x.neg().cuda(), slots)
+    dead = torch.zeros(6, 2, dtype=torch.bool)
+    dead[1, 0] = dead[2, 1] = dead[3, 0] = True
+    for got, want in zip(tq.kv_read(c, slots, bf16=True), (x, x.neg())):
+        got, want = got.cpu().double(), want.double()
+        alive = int((~got[dead].isnan()).sum())
+        assert alive == 0
+        step = want.abs().amax(-1, keepdim=True) / top
+        # half a code (8 bits: of the largest binade, 32 steps of its scale), the scale's and the result's rounding
+        bound = step * (0.5 if kind == "4" else 16.0) + want.abs() * 2.0 ** -7 + step * 2.0 ** -9
+        assert ((got - want).abs() <= bound)[~dead].all()
