@@ -366,7 +366,7 @@ tq_status tq_qk_norm_rope(const tq_norm_rope *p, const tq_head_rows *q, const tq
 /* Key and value rows [tokens, kv_heads, head_dim] into the cache, one launch.
  *   slots  [tokens] int64; a token whose slot is negative or past the cache is not
  *          written; slots of one call are distinct (a slot given twice holds
- *          either token's row)
+ *          parts of either token's row, and a scale of either)
  * With 16 bits dtype is the cache's.  tokens == 0 is a no-op; limits as above for
  * rows = 2 * tokens * kv_heads.  Errors as above, TQ_ERR_BUFFER for a cache with unsupported
  * sizes. */

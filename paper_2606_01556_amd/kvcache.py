@@ -184,7 +184,8 @@ def rope_table(max_positions: int, rotary_dim: int, base: float = 10000.0, devic
 def kv_append(cache: KVCache, k, v, slots, stream=None) -> None:
     """k and v [tokens, kv_heads, head_dim] into the cache at slots [tokens] int64,
     quantized where it has 8 or 4 bits (tq_kv_append).  A token whose slot is
-    negative is not written; slots of one call are distinct."""
+    negative or past the cache is not written; slots of one call are distinct (rows
+    written twice are a mixture of both)."""
     c = _handle(cache)
     call = lambda dev, st: _native.append(c, k, v, slots, dev, st)
     if stream is not None:
