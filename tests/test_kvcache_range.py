@@ -143,3 +143,22 @@ def test_rows_past_the_largest_scale(kind, top, d):
         # half a code (8 bits: of the largest binade, 32 steps of its scale), the scale's and the result's rounding
         bound = step * (0.5 if kind == "4" else 16.0) + want.abs() * 2.0 ** -7 + step * 2.0 ** -9
         assert ((got - want).abs() <= bound)[~dead].all()
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS[:2])
+@pytest.mark.parametrize("lens", [[40, 9], [5000, 33]])
+def test_infinite_values(kind, dtype, lens):
+    """A live value that is infinite leaves no finite number in its channel, and all
+    others as they were."""
+    s = Held(lens, 2, 128, 16, kind, dtype, seed=2)
+    k, v = randn(sum(lens), 2, 128, seed=1), randn(sum(lens), 2, 128, seed=2)
+    q = randn(2, 8, 128, seed=3).to(dtype)
+    refill(s, k, v, dtype)
+    clean, clean_lse = run(s, q)
+    v[5, 0, 17], v[7, 1, 100], v[lens[0] - 1, 1, 3] = math.inf, -math.inf, math.inf
+    refill(s, k, v, dtype)
+    got, lse = run(s, q)
+    hit = np.zeros(got.shape, bool)
+    hit[0, :4, 17] = hit[0, 4:, 100] = hit[0, 4:, 3] = True
+    assert not np.isfinite(got[hit]).any() and np.array_equal(got[~hit], clean[~hit])
+    assert np.array_equal(lse, clean_lse)
