@@ -406,9 +406,9 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
  *               aligned, free again when the stream has run the call; may be NULL
  *               where that size is 0 (short streams)
  * What slots outside a stream's range hold (NaN too) has no effect.  A value of its
- * range that is NaN or infinite makes its channel NaN (an infinite one too, as weights
- * enter the products in parts, of which some are zero).  Scores, the
- * softmax and the sums are fp32; the softmax's weights enter the products with v with
+ * range that is not finite leaves its channel (8 and 4 bits: its row's channels) without a
+ * finite number; an infinity may come out as NaN, since weights enter the products in
+ * parts, of which some are zero.  Scores, the softmax and the sums are fp32; the softmax's weights enter the products with v with
  * all their bits (16-bit cache of bf16 values) or with 22, or to 2^-37 of the largest
  * weight (else).  One launch for short streams, else two; the result does not
  * depend on timing.  batch == 0 is a no-op; batch <= 65535, max_pages
