@@ -1,7 +1,8 @@
-"""Build libtq.so (the HIP kernels and the C ABI) in place for gfx950, and _tqtorch.so
-(the native half of kvcache.py, against torch)."""
+"""Build libtq.so (the HIP kernels and the C ABI) in place for gfx950, and, where a PyTorch
+for ROCm is installed, _tqtorch.so (the native half of kvcache.py, against it)."""
 import glob
 import os
+import shutil
 import subprocess
 import sysconfig
 
@@ -9,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libtq.so")
 BINDING = os.path.join(HERE, "_tqtorch.so")
-CXX = os.environ.get("CXX", "g++")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+# any C++ compiler for the host: without g++ the one that comes with hipcc
+CXX = os.environ.get("CXX") or shutil.which("g++") or os.path.join(os.path.dirname(HIPCC), "amdclang++")
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -33,8 +35,20 @@ def build(verbose: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(LIB + ".tmp", LIB)
-    build_binding(verbose)
+    if has_torch():
+        build_binding(verbose)
+    else:
+        print("no PyTorch for ROCm here: libtq.so only, without _tqtorch.so", flush=True)
     return LIB
+
+
+def has_torch() -> bool:
+    """Whether the binding has something to be built against (the C library needs none)."""
+    try:
+        import torch
+    except ImportError:
+        return False
+    return torch.version.hip is not None
 
 
 def build_binding(verbose: bool = False) -> str:
