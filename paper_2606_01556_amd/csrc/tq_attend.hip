@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     // Q^T: column r, the values of the runs a key lane loads; c1: what a score's
     // product with the key's scale is multiplied by, log2(e) |scale| (its sign goes to Q)
     u32x4 q[KS];
-    const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f) * (SK ? kSmall : 1.0f);     // (-infinity times it has to stay so)
+    const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f) * (SK ? kSmall : 1.0f);  // (-infinity times it has to stay so)
     {
       const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + h0 + min(wb * kHeads + r, a.group - h0 - 1)) * a.q_hs;
       const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, live = r < heads ? 0xffffffffu : 0u;

@@ -162,3 +162,17 @@ def test_infinite_values(kind, dtype, lens):
     hit[0, :4, 17] = hit[0, 4:, 100] = hit[0, 4:, 3] = True
     assert not np.isfinite(got[hit]).any() and np.array_equal(got[~hit], clean[~hit])
     assert np.array_equal(lse, clean_lse)
+
+
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -110, -2.0 ** -104])
+@pytest.mark.parametrize("lens", [[40, 9], [5000, 33]])
+def test_scales_next_to_zero(lens, scale):
+    """Products q . k far above what a scale next to zero leaves of them: the score is
+    their product also there, and zero with a scale of zero."""
+    s = Held(lens, 2, 128, 16, "bf16", BF16, seed=2)
+    refill(s, 2.0 ** 50 * randn(sum(lens), 2, 128, seed=1), randn(sum(lens), 2, 128, seed=2), BF16)
+    q = (2.0 ** 50 * randn(2, 8, 128, seed=3)).to(BF16)
+    got, lse = run(s, q, scale=scale)
+    ref, ref_lse, bound, lse_bound = s.plain(q, scale, 0)
+    over, lse_over = (np.abs(got - ref) - bound).max(), (np.abs(lse - ref_lse) - lse_bound).max()
+    assert over <= 0 and lse_over <= 0, (over, lse_over)
