@@ -41,16 +41,16 @@
 // order, so that a result does not depend on timing.  Short ranges get a work-group
 // each and need no second launch.
 //
-// Measured (d = 128, both launches, back-to-back calls; reading alone streams 512 MB at
-// 7.0 TB/s):
+// Measured (d = 128 but for the last, both launches, back-to-back calls; reading alone
+// streams 512 MB at 6.9 TB/s):
 //   1 stream of 131072 tokens, 8 kv heads, fp16              88 us, 6.1 TB/s
 //   32 streams up to 8192, bf16                              95 us, 6.1 TB/s
 //   64 streams up to 8192, 8 bits, pages of 64              101 us, 5.8 TB/s
-//   48 streams up to 16384, 4 bits, pages of 16              84 us, 5.2 TB/s
-// of which the first launch takes 81, 89, 95 and 78 us (6.2 to 6.6 TB/s of what it reads,
-// at 4 bits 9 % more than it has to: the scales of 16 tokens are 32 bytes), its
-// work-groups ending 4 to 5 us apart, and the join the rest.  At 4 bits the vector ALU
-// is 52 % busy, at 16 bits 9 %.  Without effect or worse: e4m3 products of the keys with Q split into e4m3
+//   48 streams up to 16384, 4 bits, pages of 16              85 us, 5.2 TB/s
+//   16 streams up to 4096, 8 kv heads of 256, fp16           64 us, 4.5 TB/s
+// In a kernel trace the first launch takes 84, 92, 98, 81 and 60 us (6.0 to 6.5 TB/s of what
+// it reads in the first four, at 4 bits 9 % more than it has to: the scales of 16 tokens
+// are 32 bytes) and the join 4 to 5.5, together up to 2 % more than a call takes.  At 4 bits the vector ALU is 54 % busy, at 16 bits 10 %.  Without effect or worse: e4m3 products of the keys with Q split into e4m3
 // terms (and scores off by 2^-15 of sum |q k|), eight wavefronts in one work-group, a
 // join by whichever work-group comes last (its fences drop the L2s under the others).
 #include <cfloat>
@@ -143,7 +143,7 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 __device__ __forceinline__ f2 unpack2(uint32_t w) { return __builtin_convertvector(__builtin_bit_cast(h2, w), f2); }
 
 // NB bytes from p (p aligned to min(NB, 16)).  The cache is read once per call:
-// non-temporal loads stream it at 7.0 TB/s instead of 6.2 (512 MB).
+// non-temporal loads stream it at 6.9 TB/s instead of 6.2 (512 MB).
 template <bool ONCE, typename T>
 __device__ __forceinline__ T stream_load(const uint8_t *p) {
   if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T *>(p));
@@ -800,6 +800,8 @@ AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int
   //   16 bits  512: 8.0, 8.0   768: 10.0, 8.4    1024: 17.9, 21.2   1536: 28.0, 23.9
   //    8 bits  768: 8.3, 8.3  1024:  9.7, 8.3    2048: 20.3, 22.4
   //    4 bits 1024: 8.1, 8.0  1536: 10.2, 8.3    2048: 13.1, 18.6
+  // (So at 8 bits the rule keeps a few streams of 769 to 1024 tokens in one launch, up to 1.4 us
+  // longer than runs would take.  Only d = 128 was compared.)
   const int rounds2 = 32768 / (c.d * c.bits), most_steps = (rounds2 < 32 ? rounds2 : 32) * (ranges >= kCus / 2 ? 2 : 1);
   // (and a launch numbers its lanes in 32 bits)
   p.direct = steps <= most_steps && ranges * 64 * kDirectWaves < ((int64_t)1 << 32);

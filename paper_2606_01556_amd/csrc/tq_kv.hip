@@ -8,13 +8,16 @@
 // largest value come from DPP lane swaps among its lanes.  Nothing passes through
 // LDS, and a row is read and written once.
 //
-// Measured (d = 128, bf16 rows; a copy kernel reaches 5.9 TB/s):
-//   norm and rotation of 8192 tokens of 64 + 8 heads      55 us, 5.5 TB/s
-//   the same of 2048 tokens of 32 + 8 heads and the 16-bit cache   15 us
-//   8192 tokens of 8 + 8 heads written in 8 bits 12 us, read back 10 us
+// Measured (d = 128; a copy kernel reaches 6.5 TB/s):
+//   rotation of 8192 tokens of 64 + 8 heads, fp16         55 us, 5.6 TB/s
+//   the same with norms, bf16                             59 us, 5.2 TB/s
+//   rotation of 2048 tokens of 32 + 8 heads into the 16-bit cache and read back, bf16   15 us
+//   8192 tokens of 8 + 8 heads written in 8 bits (bf16) 11 us, in 4 (fp16) 14, read back 10
+//   norm, rotation and 4-bit write of 8192 tokens of 32 + 8 heads, bf16   43 us
 // One row per lane: with two to four, whose loads would be in flight together, the
-// first takes 61 us and the last two 32.  Non-temporal stores of q and k save 2 us here
-// and cost the kernel that reads them next 2.5.
+// first takes 61 us and 8192 tokens written and read in 8 bits 32 instead of 21.
+// Non-temporal stores of q and k save 2 us here and cost the kernel that reads them next
+// 2.5.
 #include "tq_device.hpp"
 #include "tq_kv.hpp"
 
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(256) void tokens_kernel(const TokenArgs a) {
   const HeadRows &src = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
   // the lane's two runs of eight values, in the two halves of the rotated channels or
   // of the others: either is a stretch that neighbouring lanes continue (two runs side
-  // by side: 24 us instead of 22 for 8192 tokens in 8 bits, written and read back)
+  // by side: 24 us instead of 21 for 8192 tokens in 8 bits, written and read back)
   const bool turned = e < a.rot / 16;
   const int i0 = 8 * e + (turned ? 0 : a.rot / 2);
   const int i1 = 8 * e + (turned ? a.rot / 2 : D / 2);
