@@ -217,10 +217,10 @@ constexpr int lds_floats(int waves, int hb, int d, int bits, int cols) {
 template <bool BF16>
 __device__ __forceinline__ void store4(const AttendArgs &a, int d, int64_t row, int d0, float m, float l, v4f o) {
   const float inv = 1.0f / l;
-  int e;
-  const float f = frexpf(l, &e);         // (m and l's binade all but cancel: they go together first)
   *reinterpret_cast<u32x2 *>(a.out + row * d + d0) = u32x2{pack2<BF16>(o[0] * inv, o[1] * inv), pack2<BF16>(o[2] * inv, o[3] * inv)};
-  if (a.lse != nullptr && d0 == 0) a.lse[row] = (m + (float)e + log2f(f)) * (1.0f / kLog2e);
+  // (m and l's binade all but cancel: they go together first)
+  if (a.lse != nullptr && d0 == 0)
+    a.lse[row] = (m + (float)__builtin_amdgcn_frexp_expf(l) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l))) * (1.0f / kLog2e);
 }
 
 // What the first launch tells the join about a range, [batch][vheads]: the number
