@@ -423,6 +423,52 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
                              const int32_t *lengths, float scale, int window, void *out, float *lse,
                              void *scratch, void *stream);
 
+/* How a score is made of a query q at position p and the key k at position j:
+ *   s = scale * (q . k);  softcap > 0: s = softcap * tanh(s / softcap);
+ *   slopes != NULL: s -= slopes[query head] * |p - j|  (fp32 [q_heads]).
+ * window > 0: only keys j > p - window. */
+typedef struct {
+    float scale, softcap;
+    const float *slopes;
+    int32_t window;
+} tq_scores;
+
+/* Attention of many new tokens of every stream over the cache, which holds them already
+ * (prompts, chunks of prompts, tokens to verify):
+ *   out[r, h] = sum_j w_j v_j,  w = softmax over j of the scores
+ *   q           [tokens, q_heads, head_dim] of type dtype, the streams' new tokens one stream
+ *               after the other
+ *   starts      [batch + 1] int32: stream i's new tokens are rows starts[i] .. starts[i + 1] - 1
+ *               (ascending, taken into [0, tokens]).  They are the last of its lengths[i]
+ *               tokens: row r has the position p = lengths[i] - (starts[i + 1] - r).  Rows of no
+ *               stream give zeros and a log-sum-exp of -infinity
+ *   page_table, table_stride, max_pages, lengths  as in tq_paged_attention
+ *   prefix      [batch] int32 or NULL: stream i's first prefix[i] tokens are seen by all of its
+ *               rows, also by those before them
+ *   first       [tokens] int32 or NULL: the first position that a row sees (the start of its
+ *               document)
+ * A row sees key j of its stream if (j <= p or j < prefix) and j > p - window and j >= first;
+ * a row that sees nothing gives zeros and -infinity.
+ *   lse         [tokens, q_heads] fp32 or NULL
+ *   scratch     device buffer of tq_prompt_attention_scratch_bytes bytes, 16-byte aligned, free
+ *               again when the stream has run the call; may be NULL where that size is 0
+ * What a row does not see (NaN too) has no effect on it; a value that is not finite leaves its
+ * channel NaN or infinite in the rows that see it (8 and 4 bits: a scale that is NaN, all
+ * channels).  Scores, softmax and sums are fp32; a weight enters the product with v rounded
+ * once, to 11 bits (16-bit cache of bf16 values: 8), the divisor and the log-sum-exp take it
+ * unrounded.  One launch, or two where the keys of a row are split; the result does not depend
+ * on timing.  tokens == 0 is a no-op; batch from 1 to 65535 (0 with tokens == 0), max_pages *
+ * page_size <= 2^30, tokens * q_heads < 2^31, (tokens * q_heads + 128 * batch * kv_heads) / 128 < 2^24.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE, TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_BUFFER, TQ_ERR_HIP;
+ * the scratch size is 0 for arguments that would be refused. */
+size_t tq_prompt_attention_scratch_bytes(const tq_kv_cache *c, int tokens, int batch, int q_heads,
+                                         int max_pages, int window);
+tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int tokens,
+                              int batch, int q_heads, const int32_t *starts, const int32_t *page_table,
+                              int64_t table_stride, int max_pages, const int32_t *lengths,
+                              const int32_t *prefix, const int32_t *first, const tq_scores *scores, void *out,
+                              float *lse, void *scratch, void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *tq_status_string(tq_status s);
 

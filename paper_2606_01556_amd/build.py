@@ -21,6 +21,7 @@ FLAGS = [
     # matrix-core results land in VGPRs (no accumulator-register copies)
     "-mllvm", "-amdgpu-mfma-vgpr-form",
     "-Wall", "-Wno-unused-function",
+    "-parallel-jobs=8",            # the files beside each other
 ]
 
 

@@ -55,22 +55,13 @@
 // join by whichever work-group comes last (its fences drop the L2s under the others).
 #include <cfloat>
 
-#include "tq_device.hpp"
+#include "tq_attention.hpp"
 #include "tq_kernels.hpp"
 #include "tq_kv.hpp"
 
 namespace tq {
 
 namespace {
-
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef uint16_t s2 __attribute__((ext_vector_type(2)));
-typedef float f2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef const int32_t __attribute__((address_space(4))) const_i32;
 
 constexpr int kHeads = 16;                 // query heads of a product (its columns)
 constexpr int kRunWaves = 4;               // wavefronts of a work-group that holds a run of steps
@@ -91,35 +82,12 @@ __host__ __device__ constexpr int head_blocks(int group) { return group > kHeads
 constexpr int ranges_of(int group) { return (group + kHeads * head_blocks(group) - 1) / (kHeads * head_blocks(group)); }
 constexpr int range_heads(int group) { return group < kHeads * head_blocks(group) ? group : kHeads * head_blocks(group); }
 
-constexpr float kLog2e = 1.4426950408889634f;
-
-// The largest weight that a step may have (fp16's largest value), and the power of two at
-// which the largest one is put when the reference moves.
-constexpr float kTopWeight = 65504.0f, kHeadroom = 12.0f;
-// With bf16 rows, whose values fp32 itself just holds, the weights of a range of fewer than
-// 2^e tokens stay at 2^-e or below, so that no sum passes the largest value; the largest
-// weight is put kBelow binades lower.
-constexpr int kBelow = 8;
-constexpr float kLeastScale = 0x1p-24f;    // fp16's smallest number
-
 template <bool BF16>
 __device__ __forceinline__ v4f mfma16(u32x4 a, u32x4 b, v4f c) {
   if constexpr (BF16)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
-}
-
-// four e4m3 bytes times `scale` (a power of two) as two words of 16-bit values
-template <bool BF16>
-__device__ __forceinline__ void widen4(uint32_t w, float scale, uint32_t &lo, uint32_t &hi) {
-  if constexpr (BF16) {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
-  } else {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, scale, true));
-  }
 }
 
 // Bytes I of w0 and J of w1, codes as tq4_to_fp8 gives them (sign, four zeros, three bits),
@@ -132,13 +100,6 @@ __device__ __forceinline__ uint32_t small_halves(uint32_t w0, uint32_t w1) {
   return __builtin_amdgcn_perm(w1, w0, (uint32_t)(4 + J) << 24 | 0x0c0000u | I << 8 | 0x0cu);
 }
 
-// two fp32 values rounded to a word of 16-bit ones
-template <bool BF16>
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  const f2 v = {x, y};
-  if constexpr (BF16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
-  else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
-}
 // the two values of a word of fp16 ones
 __device__ __forceinline__ f2 unpack2(uint32_t w) { return __builtin_convertvector(__builtin_bit_cast(h2, w), f2); }
 
@@ -171,8 +132,6 @@ __device__ __forceinline__ float scale_of(u32x2 four, int j) {
   const uint32_t two = j < 2 ? four.x : four.y;
   return (float)__builtin_bit_cast(h2, two)[j & 1];
 }
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // The tokens [first, len) of a stream in steps from first rounded down to 16.
 struct Range {

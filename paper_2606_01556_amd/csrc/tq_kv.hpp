@@ -68,6 +68,33 @@ struct AttendArgs {
   int direct;
 };
 
+// Attention of many new tokens of every stream, or (shared) of the streams of every group over
+// the group's prefix; tokens are rows of q.
+constexpr int kPromptRows = 128;   // tokens times the group's query heads, of a work-group
+struct PromptArgs {
+  KvCache c;
+  const uint16_t *q;         // [tokens][hq][d]
+  int64_t q_ts, q_hs;
+  int tokens, hq, group, batch;
+  const int32_t *starts;     // [batch + 1] first rows of the streams (groups)
+  const int32_t *table;      // [batch][table_stride] page numbers
+  int64_t table_stride;
+  int max_pages;
+  const int32_t *lengths;    // [batch]
+  const int32_t *own;        // shared: [tokens] tokens behind the prefix
+  const int32_t *prefix, *first;   // [batch], [tokens], or null
+  float scale, cap;          // cap 0: none
+  const float *slopes;       // [hq] or null
+  int window;                // 0: none
+  bool shared;
+  uint16_t *out;             // [tokens][hq][d]
+  float *lse;                // [tokens][hq] or null
+  // parts where splits > 1 or shared: [splits][tokens][hq] references and sums, then as many products [d]
+  float *scratch;
+  int tiles, splits;
+  int64_t blocks;
+};
+
 hipError_t launch_tokens(const TokenArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_kv_read(const ReadArgs &a, bool bf16, hipStream_t s);
 // How an attention call is cut, by what the host knows of it: direct, one
@@ -80,6 +107,19 @@ struct AttendPlan {
 };
 AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window);
 hipError_t launch_attend(const AttendArgs &a, bool bf16, hipStream_t s);
+
+// How an attention of many tokens is cut: row tiles (a bound over all streams) and parts of
+// a tile's keys.
+struct PromptPlan {
+  int tiles, splits;
+  int64_t blocks;
+  size_t scratch;            // bytes
+};
+PromptPlan prompt_plan(const KvCache &c, int tokens, int batch, int hq, int64_t max_len, int window, bool shared);
+hipError_t launch_prompt(const PromptArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_prompt_64(const PromptArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_prompt_128(const PromptArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_prompt_256(const PromptArgs &a, bool bf16, hipStream_t s);
 
 // row / d for 0 <= row < 2^31 and 2 <= d < 2^31: with L = ceil(log2 d) and
 // magic = ceil(2^(31 + L) / d) <= 2^32 - 1 (2^31 where d is a power of two), the

@@ -213,4 +213,62 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
   return hip_status(tq::launch_attend(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
+// the scores of a call
+static tq_status check_scores(const tq_scores *s) {
+  if (s == nullptr) return TQ_ERR_NULL;
+  if (!std::isfinite(s->scale) || !std::isfinite(s->softcap) || s->softcap < 0.0f || s->window < 0) return TQ_ERR_SHAPE;
+  if (!aligned(s->slopes, 4)) return TQ_ERR_ALIGN;
+  return TQ_OK;
+}
+
+static tq_status plan_prompt(const tq_kv_cache *c, const tq::KvCache &k, int tokens, int batch, int q_heads, int max_pages,
+                             int window, bool shared, tq::PromptPlan &p) {
+  if (tokens < 0 || batch < 0 || batch > 65535 || (batch == 0 && tokens > 0) || q_heads < 1 || q_heads > 65535 ||
+      q_heads % c->kv_heads != 0 || max_pages < 1 || (int64_t)max_pages * c->page_size > ((int64_t)1 << 30) || window < 0 ||
+      (int64_t)tokens * q_heads >= ((int64_t)1 << 31))
+    return TQ_ERR_SHAPE;
+  p = tq::prompt_plan(k, tokens, batch, q_heads, (int64_t)max_pages * c->page_size, window, shared);
+  // (a launch numbers its lanes in 32 bits)
+  return p.blocks < ((int64_t)1 << 24) ? TQ_OK : TQ_ERR_SHAPE;
+}
+
+size_t tq_prompt_attention_scratch_bytes(const tq_kv_cache *c, int tokens, int batch, int q_heads, int max_pages, int window) {
+  tq::KvCache k;
+  tq::PromptPlan p;
+  if (check_cache(c, k) != TQ_OK || plan_prompt(c, k, tokens, batch, q_heads, max_pages, window, false, p) != TQ_OK) return 0;
+  return p.scratch;
+}
+
+tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int tokens, int batch, int q_heads,
+                              const int32_t *starts, const int32_t *page_table, int64_t table_stride, int max_pages,
+                              const int32_t *lengths, const int32_t *prefix, const int32_t *first, const tq_scores *scores,
+                              void *out, float *lse, void *scratch, void *stream) {
+  tq::PromptArgs a = {};
+  if (starts == nullptr || page_table == nullptr || lengths == nullptr || out == nullptr) return TQ_ERR_NULL;
+  TQ_TRY(check_cache(c, a.c));
+  tq::HeadRows rows;
+  TQ_TRY(check_rows(q, rows));
+  TQ_TRY(check_scores(scores));
+  tq::PromptPlan p;
+  TQ_TRY(plan_prompt(c, a.c, tokens, batch, q_heads, max_pages, scores->window, false, p));
+  if (table_stride < 0) return TQ_ERR_SHAPE;
+  if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
+  if (!aligned(starts, 4) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(prefix, 4) || !aligned(first, 4) ||
+      !aligned16(out) || !aligned(lse, 4) || !aligned16(scratch))
+    return TQ_ERR_ALIGN;
+  if (tokens == 0) return TQ_OK;
+  if (p.scratch != 0 && scratch == nullptr) return TQ_ERR_NULL;
+  a.q = rows.p; a.q_ts = rows.ts; a.q_hs = rows.hs;
+  a.tokens = tokens; a.hq = q_heads; a.group = q_heads / c->kv_heads; a.batch = batch;
+  a.starts = starts;
+  a.table = page_table; a.table_stride = table_stride; a.max_pages = max_pages;
+  a.lengths = lengths; a.prefix = prefix; a.first = first;
+  a.scale = scores->scale; a.cap = scores->softcap; a.slopes = scores->slopes; a.window = scores->window;
+  a.out = static_cast<uint16_t *>(out);
+  a.lse = lse;
+  a.scratch = static_cast<float *>(scratch);
+  a.tiles = p.tiles; a.splits = p.splits; a.blocks = p.blocks;
+  return hip_status(tq::launch_prompt(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

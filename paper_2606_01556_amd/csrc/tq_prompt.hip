@@ -1,0 +1,91 @@
+// Attention of many tokens: how a call is cut, and the join of the parts of rows whose keys
+// several work-groups share.
+#include "tq_attention.hpp"
+#include "tq_kernels.hpp"
+#include "tq_kv.hpp"
+
+namespace tq {
+
+namespace {
+
+constexpr int kJoinThreads = 256, kCus = 256;
+
+// A row's parts, joined: D / 4 lanes hold a row's products, `side` groups of them take its
+// parts in turn and are joined in their order, so that every sum has one order.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const PromptArgs a, int side) {
+  constexpr int Q = D / 4, GROUPS = kJoinThreads / Q;
+  __shared__ __attribute__((aligned(16))) float lds_o[GROUPS][D], lds_ml[GROUPS][2];
+  const int g = threadIdx.x / Q, d0 = 4 * (threadIdx.x % Q), mine = g % side;
+  const int64_t heads = (int64_t)a.tokens * a.hq, row = (int64_t)blockIdx.x * (GROUPS / side) + g / side;
+  const int begin = min(max(a.starts[0], 0), a.tokens), end = min(max(a.starts[a.batch], 0), a.tokens);
+  const bool live = row >= (int64_t)begin * a.hq && row < (int64_t)end * a.hq;     // (the others are cleared)
+  float m = -INFINITY, l = 0.0f;
+  v4f o = {0, 0, 0, 0};
+  auto add = [&](f2 ml, v4f y) {
+    const float m1 = fmaxf(m, ml.x);            // (of a part: finite)
+    const float f0 = __builtin_amdgcn_exp2f(m - m1), f1 = __builtin_amdgcn_exp2f(ml.x - m1);
+    m = m1;
+    l = l * f0 + ml.y * f1;
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = o[i] * f0 + y[i] * f1;
+  };
+  if (live) {
+    const float *const parts = a.scratch + 2 * a.splits * heads;
+#pragma unroll 4
+    for (int k = mine; k < a.splits; k += side)
+      add(*reinterpret_cast<const f2 *>(a.scratch + 2 * (k * heads + row)), *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
+    *reinterpret_cast<v4f *>(&lds_o[g][d0]) = o;
+    if (d0 == 0) *reinterpret_cast<f2 *>(lds_ml[g]) = f2{m, l};
+  }
+  __syncthreads();
+  if (!live || mine != 0) return;
+  for (int k = 1; k < side; k++)
+    if (k < a.splits) add(*reinterpret_cast<const f2 *>(lds_ml[g + k]), *reinterpret_cast<const v4f *>(&lds_o[g + k][d0]));
+  const bool none = l == 0.0f;
+  const float inv = 1.0f / l;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; i++) y[i] = none ? 0.0f : o[i] * inv;
+  *reinterpret_cast<u32x2 *>(a.out + row * D + d0) = u32x2{pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3])};
+  if (a.lse != nullptr && d0 == 0) a.lse[row] = none ? -INFINITY : log_sum(m, l);
+}
+
+template <int D>
+hipError_t join_rows(const PromptArgs &a, bool bf16, hipStream_t s) {
+  constexpr int GROUPS = kJoinThreads / (D / 4);
+  int side = 1;
+  while (side < a.splits && side < GROUPS) side *= 2;
+  const int64_t heads = (int64_t)a.tokens * a.hq, each = GROUPS / side;
+  const dim3 grid((uint32_t)((heads + each - 1) / each));
+  if (bf16) hipLaunchKernelGGL((join_rows_kernel<D, true>), grid, dim3(kJoinThreads), 0, s, a, side);
+  else hipLaunchKernelGGL((join_rows_kernel<D, false>), grid, dim3(kJoinThreads), 0, s, a, side);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+PromptPlan prompt_plan(const KvCache &c, int tokens, int batch, int hq, int64_t max_len, int window, bool shared) {
+  PromptPlan p;
+  const int64_t tiles = (int64_t)tokens * (hq / c.heads) / kPromptRows + batch;
+  const int64_t units = tiles * c.heads;
+  // Where the tiles leave CUs without work, a tile's keys are split, down to 256 of them.
+  const int64_t room = kCus * (c.d == 256 ? 1 : c.d == 128 ? 2 : 3);
+  const int64_t longest = window > 0 && (int64_t)window + tokens < max_len ? (int64_t)window + tokens : max_len;
+  int64_t splits = units > 0 ? room / units : 1;
+  if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
+  if (splits < 1) splits = 1;
+  p.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
+  p.splits = (int)splits;
+  p.blocks = units * splits;
+  p.scratch = splits > 1 || shared ? (size_t)splits * tokens * hq * (2 + c.d) * sizeof(float) : 0;
+  return p;
+}
+
+hipError_t launch_prompt(const PromptArgs &a, bool bf16, hipStream_t s) {
+  const hipError_t e = a.c.d == 64 ? launch_prompt_64(a, bf16, s) : a.c.d == 128 ? launch_prompt_128(a, bf16, s) : launch_prompt_256(a, bf16, s);
+  if (e != hipSuccess || a.splits == 1 || a.shared) return e;
+  return a.c.d == 64 ? join_rows<64>(a, bf16, s) : a.c.d == 128 ? join_rows<128>(a, bf16, s) : join_rows<256>(a, bf16, s);
+}
+
+}  // namespace tq

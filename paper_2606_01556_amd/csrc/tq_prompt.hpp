@@ -1,0 +1,587 @@
+// Attention of many new tokens over the paged cache (prompts, chunks of prompts, tokens to
+// verify), and of a batch's tokens over a prefix that they share:
+//
+//   o_r = sum_j softmax_j(s_rj) v_j,  s_rj = cap tanh(scale q_r . k_j / cap) - slope |p_r - j|,
+//   j in [lo_r, hi_r)
+//
+// (cap and slope or neither).  Every mask that a call can ask for (causal, window, prefix,
+// documents) leaves a row one interval, so the kernel knows two numbers a row and no mask.
+//
+// A row r is a new token and one of the query heads of a key-value head's group: a work-group
+// holds 128 rows of one key-value head, 32 to a wavefront, and runs over the keys in tiles of
+// 64, which it stages in LDS for its four wavefronts.
+//
+//  * S^T = K Q^T in 32x32x16 products with the rows as columns: a lane holds scores of one
+//    row (lane % 32) for keys 8 i + 4 (lane / 32) + (0 .. 3).  What a row needs (its interval,
+//    reference, sum) is one register, and a tile's largest weight is a maximum within lanes.
+//  * Two such runs of four keys, exponentiated and rounded, are the second operand of
+//    O^T = V^T P^T as they stand: which keys make up a product is free as long as V^T's operand
+//    takes the same, and LDS reads it transposed, four keys of a channel at a time.
+//  * The reference of the softmax moves only when a weight passes 65504 (bf16 rows: 1 over the
+//    number of keys), as in the attention of one token: most tiles neither exchange
+//    anything between lanes nor scale what has been summed.
+//  * A weight is rounded once to the second product's type (fp16: 2^-12 of itself at most, and
+//    2^-36 of the largest one; bf16 rows, whose values may pass fp16's range: 2^-9).  The
+//    products are what bounds the kernel, and more terms of a weight would be more products;
+//    the roundings of different keys are independent and stay below the result's own.  The
+//    sum that divides, and the log-sum-exp, take the weights unrounded, in fp32.
+//  * Rows of 16 bits go from memory to LDS directly, 16 bytes a lane, swizzled by the address
+//    that a lane reads (so that neither kind of LDS read has bank conflicts); codes are
+//    widened on their way, exactly, their scales apply to scores and weights in fp32.
+//  * A tile's loads are in flight while the tile before it is computed on.
+//
+// Keys that a row does not see have no part in it, whatever they hold: a tile in which any
+// row's interval ends is searched for infinities and NaN, and where there is one the values
+// enter the product without it, and the rows that do see it get a NaN by a second product.
+#pragma once
+
+#include <cfloat>
+
+#include "tq_attention.hpp"
+#include "tq_kernels.hpp"
+#include "tq_kv.hpp"
+
+namespace tq {
+
+namespace {
+
+constexpr int kPromptWaves = 4, kPromptThreads = 64 * kPromptWaves;
+constexpr int kTileKeys = 64;
+constexpr float kTopBinades = 15.99f;      // 2^15.99 < 65504
+
+// wavefronts of a SIMD that the registers are cut for
+constexpr int prompt_occupancy(int d) { return d == 256 ? 1 : d == 128 ? 2 : 3; }
+
+// bytes of LDS: two stages of keys, values and (codes) their scales; four pairs of bounds and a flag
+constexpr int prompt_stage(int d, int bits) { return kTileKeys * d * 4 + (bits < 16 ? kTileKeys * 12 + 16 : 0); }
+constexpr int prompt_lds_bytes(int d, int bits) { return 2 * prompt_stage(d, bits) + 64 * kPromptWaves; }
+
+template <bool BF16>
+__device__ __forceinline__ v16f mfma32(u32x4 a, u32x4 b, v16f c) {
+  if constexpr (BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+
+// 16 bytes per lane from sbase + voff into LDS at lds + 16 * lane
+__device__ __forceinline__ void load_to_lds(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds) : "memory");
+}
+// this wavefront's loads and LDS accesses done, then all wavefronts'
+__device__ __forceinline__ void wait_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+// Four 16-bit values of one column: of 16 lanes, lanes 4 r .. 4 r + 3 address row r's 16 values,
+// and lane i gets column i of the four rows.
+__device__ __forceinline__ u32x2 read_columns(const uint8_t *p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)p));
+}
+
+// the halves of w whose exponent is all ones, as their top bits
+template <bool BF16>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  return BF16 ? ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+}
+
+struct Interval {
+  int lo, hi;    // empty: INT32_MAX and 0
+};
+
+template <int D, int BITS, bool BF16, bool EXT>
+__global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_kernel(const PromptArgs a) {
+  constexpr int KT = kTileKeys, W = kPromptWaves, T = kPromptThreads;
+  constexpr int RB = D * BITS / 8;              // bytes of a cache row
+  constexpr int LB = D * 2, LC = LB / 16;       // bytes and 16-byte pieces of a row in LDS
+  constexpr int KS = D / 16, DT = D / 32, NK = KT / 32;
+  constexpr bool VBF = BITS == 16 && BF16;      // type of the second product
+  constexpr int VOFF = KT * LB, SOFF = 2 * KT * LB, STAGE = prompt_stage(D, BITS);
+  constexpr uint32_t kOne = VBF ? 0x3f80u : 0x3c00u;
+
+  extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+  int *const bounds = reinterpret_cast<int *>(smem + 2 * STAGE), *const flag = bounds + 4 * W;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+  const int r32 = lane & 31, half = lane >> 5;
+  const int hkv = a.c.heads, lps = a.c.lps;
+  // tiles of the longest intervals first (a causal prompt's last ones)
+  const int kvh = blockIdx.x % hkv, unit = blockIdx.x / hkv, split = unit % a.splits;
+  const int tile = a.tiles - 1 - unit / a.splits;
+
+  auto start_of = [&](int i) -> int { return min(max(a.starts[i], 0), a.tokens); };
+  // Stream i's tiles are numbered from floor(rows before it / 128) + i: numbers enough for
+  // each, in order, without a sum over the streams.
+  auto first_tile = [&](int i) -> int { return (int)(((int64_t)start_of(i) * a.group) / kPromptRows) + i; };
+
+  // rows of no stream (in shared mode the join leaves them to the tokens' own keys)
+  if (!a.shared && threadIdx.x < 64) {
+    const int begin = start_of(0), end = start_of(a.batch), none = begin + a.tokens - end;
+    for (int i = blockIdx.x; i < none; i += gridDim.x) {
+      const int64_t row = (int64_t)(i < begin ? i : i - begin + end) * a.hq;
+      for (int e = lane; e < a.hq * (D / 2); e += 64) reinterpret_cast<uint32_t *>(a.out + row * D)[e] = 0;
+      if (a.lse != nullptr)
+        for (int e = lane; e < a.hq; e += 64) a.lse[row + e] = -INFINITY;
+    }
+  }
+
+  // the stream whose tile this is: the last with first_tile <= tile, 64 candidates at a time
+  int s = 0;
+  for (int n = a.batch; n > 1;) {
+    const int step = (n + 63) / 64, i = s + lane * step;
+    const bool before = lane * step < n && first_tile(i) <= tile;
+    const int count = max(__builtin_popcountll(__ballot(before)), 1) - 1;
+    s = uniform(s + count * step);
+    n = uniform(min(step, n - count * step));
+  }
+  const int start = uniform(start_of(s)), tokens = uniform(start_of(s + 1)) - start;
+  const int at = tile - uniform(first_tile(s));
+  const int row0 = at * kPromptRows, rows = tokens * a.group;     // < 2^31 (host)
+  if (at < 0 || row0 >= rows) return;
+
+  // this lane's row and its interval
+  const int cap = a.max_pages << lps;                             // <= 2^30 (host)
+  const int len = min(max(uniform(a.lengths[s]), 0), cap);
+  const bool live = row0 + 32 * w < rows;                         // the wavefront holds rows
+  const int row = min(row0 + 32 * w + r32, rows - 1);
+  const int token = (int)((uint32_t)row / (uint32_t)a.group), head = kvh * a.group + (row - token * a.group);
+  int pos;
+  Interval seen;
+  if (a.shared) {
+    const int own = min(max(a.own[start + token], 0), 1 << 30);
+    pos = len + own - 1;
+    seen = {0, len};
+  } else {
+    pos = len - tokens + token;
+    seen = {0, max(pos + 1, 0)};
+    if (a.prefix != nullptr) seen.hi = max(seen.hi, min(a.prefix[s], len));
+    if (a.window > 0 && pos >= a.window) seen.lo = pos - a.window + 1;
+    if (a.first != nullptr) seen.lo = max(seen.lo, a.first[start + token]);
+  }
+  if (seen.lo >= seen.hi) seen = {INT32_MAX, 0};
+
+  // bounds of the wavefront's rows, and of all rows
+  int lo_min = seen.lo, lo_max = seen.lo, hi_min = seen.hi, hi_max = seen.hi;
+#pragma unroll
+  for (int m = 1; m < 32; m <<= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, m)); lo_max = max(lo_max, __shfl_xor(lo_max, m));
+    hi_min = min(hi_min, __shfl_xor(hi_min, m)); hi_max = max(hi_max, __shfl_xor(hi_max, m));
+  }
+  lo_min = uniform(lo_min); lo_max = uniform(lo_max); hi_min = uniform(hi_min); hi_max = uniform(hi_max);
+  if (lane == 0) {
+    bounds[4 * w] = lo_min; bounds[4 * w + 1] = lo_max; bounds[4 * w + 2] = hi_min; bounds[4 * w + 3] = hi_max;
+    if (w == 0) *flag = 0;
+  }
+
+  // Q^T: column r32, values 16 k + 8 half ...  (the scale's sign goes to Q)
+  u32x4 q[KS];
+  {
+    const uint16_t *qp = a.q + (int64_t)(start + token) * a.q_ts + (int64_t)head * a.q_hs + 8 * half;
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int k = 0; k < KS; k++) {
+      q[k] = *reinterpret_cast<const u32x4 *>(qp + 16 * k);
+#pragma unroll
+      for (int i = 0; i < 4; i++) q[k][i] ^= flip;
+    }
+  }
+  __syncthreads();
+  int all_lo = INT32_MAX, all_lo_max = 0, all_hi_min = INT32_MAX, all_hi = 0;
+#pragma unroll
+  for (int i = 0; i < W; i++) {
+    all_lo = min(all_lo, bounds[4 * i]); all_lo_max = max(all_lo_max, bounds[4 * i + 1]);
+    all_hi_min = min(all_hi_min, bounds[4 * i + 2]); all_hi = max(all_hi, bounds[4 * i + 3]);
+  }
+  all_lo = uniform(all_lo); all_lo_max = uniform(all_lo_max); all_hi_min = uniform(all_hi_min); all_hi = uniform(all_hi);
+
+  // this split's keys [k0, k1), from a multiple of 64
+  int k0 = 0, k1 = 0;
+  if (all_lo < all_hi) {
+    const int base = all_lo & ~(KT - 1), n = (all_hi - base + KT - 1) / KT;
+    k0 = base + (int)((int64_t)n * split / a.splits) * KT;
+    k1 = min(base + (int)((int64_t)n * (split + 1) / a.splits) * KT, all_hi);
+  }
+
+  // what a score's product with the key's scale is multiplied by, in binades
+  const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f);     // (-infinity times it has to stay so)
+  const float cap_in = EXT && a.cap > 0.0f ? 2.0f * kLog2e * (fabsf(a.scale) / a.cap) : 0.0f, cap_out = a.cap * kLog2e;
+  const float slope = EXT && a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.0f;
+  // binades above the reference at which it has to move, and where it puts the largest weight
+  float most = kTopBinades, headroom = kHeadroom;
+  if constexpr (VBF) {
+    most = (float)(__builtin_clz(max(len, 1)) - 32);
+    headroom = most - kBelow;
+  }
+
+  v16f o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; i++) o[i] = v16f{0};
+  float m = -FLT_MAX, l = 0.0f;      // (finite: keys whose score is -infinity have the weight 0 also before the first other one)
+
+  // ---- loads.  A wavefront's load takes rows of one page (up to 16 rows); keys outside the
+  // rows' intervals take the nearest one's row.
+  const_i32 *const pages = (const_i32 *)(a.table + s * a.table_stride);
+  auto held = [&](int key) -> int { return min(max(key, all_lo), all_hi - 1); };
+  constexpr int PIECE = BITS == 16 ? 16 : KT * RB / T < 16 ? KT * RB / T : 16;    // bytes of a lane's load
+  constexpr int PR = RB / PIECE, LR = 64 / PR, NL = KT / (LR * W);                // lanes of a row, rows of a load, loads
+  static_assert(LR <= 16 && NL >= 1 && NL * LR * W == KT);
+  const int lrow = lane / PR, lpiece = lane % PR;
+  int page[NL];
+  auto load_pages = [&](int k) {
+#pragma unroll
+    for (int i = 0; i < NL; i++) page[i] = pages[held(k + (i * W + w) * LR) >> lps];
+  };
+  auto base_of = [&](int i) -> int64_t { return ((int64_t)min(max(page[i], 0), a.c.pages - 1) * hkv + kvh) << lps; };
+  u32x4 kraw[BITS < 16 ? NL : 1], vraw[BITS < 16 ? NL : 1];       // codes on their way
+  uint16_t sraw = 0;
+  auto load = [&](int k, uint32_t stage) {
+#pragma unroll
+    for (int i = 0; i < NL; i++) {
+      const int64_t base = base_of(i) * RB;
+      const int r = (i * W + w) * LR + lrow;
+      const uint32_t off = (uint32_t)(held(k + r) & ((1 << lps) - 1)) * RB;
+      if constexpr (BITS == 16) {
+        const uint32_t to = stage + (i * W + w) * 1024;
+        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? r & 15 : r & 7)), a.c.k + base, lds0 + to);
+        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3))), a.c.v + base, lds0 + to + VOFF);
+      } else if constexpr (PIECE == 16) {
+        kraw[i] = *reinterpret_cast<const u32x4 *>(a.c.k + base + off + 16 * lpiece);
+        vraw[i] = *reinterpret_cast<const u32x4 *>(a.c.v + base + off + 16 * lpiece);
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(a.c.k + base + off + 8 * lpiece);
+        const u32x2 y = *reinterpret_cast<const u32x2 *>(a.c.v + base + off + 8 * lpiece);
+        kraw[i] = u32x4{x.x, x.y, 0, 0};
+        vraw[i] = u32x4{y.x, y.y, 0, 0};
+      }
+    }
+    if constexpr (BITS < 16) {
+      // (wavefront 0 the keys' scales, 1 the values')
+      if (w < 2) {
+        const int key = held(k + lane);
+        const int64_t p = min(max(pages[key >> lps], 0), a.c.pages - 1);
+        sraw = (w == 0 ? a.c.ks : a.c.vs)[((p * hkv + kvh) << lps) + (key & ((1 << lps) - 1))];
+      }
+    }
+  };
+  // codes as 16-bit values in LDS: keys in Q's type, values in fp16
+  auto widen = [&](uint32_t stage) {
+    if constexpr (BITS < 16) {
+      constexpr int WORDS = PIECE / 4, PER = BITS == 8 ? 2 : 1;   // words of a piece, words of 8 codes
+#pragma unroll
+      for (int i = 0; i < NL; i++) {
+        const int r = (i * W + w) * LR + lrow;
+#pragma unroll
+        for (int e = 0; e < WORDS / PER; e++) {
+          const int c = lpiece * (WORDS / PER) + e;
+          auto eight = [&](const u32x4 &raw, auto bf) -> u32x4 {
+            constexpr bool TO = decltype(bf)::value;
+            uint32_t w0, w1, y0, y1, y2, y3;
+            if constexpr (BITS == 8) { w0 = raw[2 * e]; w1 = raw[2 * e + 1]; }
+            else tq4_to_fp8(raw[e], w0, w1);
+            widen4<TO>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+            widen4<TO>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+            return u32x4{y0, y1, y2, y3};
+          };
+          *reinterpret_cast<u32x4 *>(smem + stage + r * LB + 16 * (c ^ (LC > 8 ? r & 15 : r & 7))) =
+              eight(kraw[i], std::integral_constant<bool, BF16>());
+          *reinterpret_cast<u32x4 *>(smem + stage + VOFF + r * LB + 16 * (c ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3)))) =
+              eight(vraw[i], std::integral_constant<bool, false>());
+        }
+      }
+      // the keys' scales; the values' as binades and their inverse.  (A value scale of zero, whose
+      // codes are zero, counts as fp16's smallest, and so does NaN, whose row is marked.)
+      float *const to = reinterpret_cast<float *>(smem + stage + SOFF) + lane;
+      const float x = half_bits_to_float(sraw);
+      if (w == 0) {
+        to[0] = x;
+      } else if (w == 1) {
+        const float y = fmaxf(x, kLeastScale);
+        to[KT] = __builtin_amdgcn_logf(y);
+        to[2 * KT] = 1.0f / y;
+        const uint64_t nan = __ballot(x != x);
+        if (lane == 0) *reinterpret_cast<uint64_t *>(smem + stage + SOFF + 12 * KT) = nan;
+      }
+    }
+  };
+
+  // ---- addresses of the two kinds of LDS reads
+  const uint32_t kx = LC > 8 ? lane & 15 : lane & 7;
+  const uint32_t krow = r32 * LB;
+  const int tq = lane >> 4, ti = lane & 15;
+  const int vr = 4 * (tq >> 1) + (ti >> 2);
+  const uint32_t vx = LC > 8 ? 2 * (vr & 7) : 2 * (vr & 3);
+  const uint32_t vrow = vr * LB + (ti & 1) * 8, vc = 2 * (tq & 1) + ((ti & 3) >> 1);
+
+  v16f sc[NK];
+  u32x4 pt[NK][2];
+  auto key_of = [&](int i, int v) -> int { return 32 * i + 8 * (v >> 2) + 4 * half + (v & 3); };
+  auto scores = [&](int k, uint32_t stage) {
+#pragma unroll
+    for (int i = 0; i < NK; i++) {
+      sc[i] = v16f{0};
+#pragma unroll
+      for (int e = 0; e < KS; e++) {
+        const u32x4 op = *reinterpret_cast<const u32x4 *>(smem + stage + 32 * i * LB + krow + 16 * ((2 * e + half) ^ kx));
+        sc[i] = mfma32<BF16>(op, q[e], sc[i]);
+      }
+      if constexpr (BITS < 16) {
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          const v4f ks = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * key_of(i, 4 * g));
+#pragma unroll
+          for (int j = 0; j < 4; j++) sc[i][4 * g + j] *= ks[j];
+        }
+      }
+    }
+    if constexpr (EXT) {
+      if (a.cap > 0.0f) {
+        // cap tanh x = cap (1 - 2 / (e^2x + 1)), good to 2^-23 of the cap
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) {
+            const float e = __builtin_amdgcn_exp2f(sc[i][v] * cap_in);
+            sc[i][v] = fmaf(__builtin_amdgcn_rcpf(e + 1.0f), -2.0f * cap_out, cap_out);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) sc[i][v] *= c1;
+      }
+      if (a.slopes != nullptr) {
+        const float far = (float)(k + 4 * half - pos);
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) sc[i][v] = fmaf(-slope, fabsf(far + (float)(32 * i + 8 * (v >> 2) + (v & 3))), sc[i][v]);
+      }
+    }
+  };
+  const uint32_t count = (uint32_t)max(seen.hi - max(seen.lo, 0), 0) & (seen.lo < seen.hi ? 0xffffffffu : 0u);
+  auto masked = [&](int k, int i, int v) -> bool { return (uint32_t)(k + key_of(i, v) - seen.lo) >= count; };
+  // the weights of the tile, rounded, in pt; edge: some row does not see all of its keys
+  auto softmax = [&](int k, uint32_t stage, bool edge) {
+    if (edge) {
+      asm volatile("");          // (a branch)
+#pragma unroll
+      for (int i = 0; i < NK; i++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) sc[i][v] = masked(k, i, v) ? -INFINITY : sc[i][v];
+    }
+    // scores in binades above no reference yet, values' scales among them: t = s + log2(scale)
+    float y = -INFINITY;
+    if constexpr (BITS < 16) {
+#pragma unroll
+      for (int i = 0; i < NK; i++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          const v4f x = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * (KT + key_of(i, 4 * g)));
+#pragma unroll
+          for (int j = 0; j < 4; j++) sc[i][4 * g + j] = EXT ? sc[i][4 * g + j] + x[j] : fmaf(sc[i][4 * g + j], c1, x[j]);
+        }
+    }
+    constexpr bool BINADES = EXT || BITS < 16;
+#pragma unroll
+    for (int i = 0; i < NK; i++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) y = fmaxf(y, sc[i][v]);
+    if constexpr (!BINADES) y *= c1;
+    if (__any(y - m > most)) {   // (also the first finite score)
+      // (only that row's: what a row gives does not depend on the rows beside it)
+      y = fmaxf(y, __shfl_xor(y, 32));
+      const float m1 = y - m > most ? y - headroom : m;
+      const float f = __builtin_amdgcn_exp2f(m - m1);
+      m = m1;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < DT; i++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) o[i][v] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < NK; i++)
+#pragma unroll
+      for (int v = 0; v < 16; v++) sc[i][v] = __builtin_amdgcn_exp2f(BINADES ? sc[i][v] - m : fmaf(sc[i][v], c1, -m));
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NK; i++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        if constexpr (BITS < 16) {
+          const v4f x = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * (2 * KT + key_of(i, 4 * g)));
+#pragma unroll
+          for (int j = 0; j < 4; j++) sum = fmaf(sc[i][4 * g + j], x[j], sum);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; j++) sum += sc[i][4 * g + j];
+        }
+      }
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < NK; i++)
+#pragma unroll
+      for (int t = 0; t < 2; t++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) pt[i][t][j] = pack2<VBF>(sc[i][8 * t + 2 * j], sc[i][8 * t + 2 * j + 1]);
+  };
+  auto values_of = [&](uint32_t at_lds, int i, int t, int c) -> u32x4 {
+    const uint8_t *p = smem + at_lds + (32 * i + 16 * t) * LB + vrow + 16 * ((4 * c + vc) ^ vx);
+    const u32x2 x = read_columns(p), y = read_columns(p + 8 * LB);
+    return u32x4{x.x, x.y, y.x, y.y};
+  };
+  auto products = [&](uint32_t at_lds) {
+#pragma unroll
+    for (int c = 0; c < DT; c++)
+#pragma unroll
+      for (int i = 0; i < NK; i++)
+#pragma unroll
+        for (int t = 0; t < 2; t++) o[c] = mfma32<VBF>(values_of(at_lds, i, t, c), pt[i][t], o[c]);
+  };
+
+  // ---- the tiles
+  if (k0 < k1) {
+    load_pages(k0);
+    load(k0, 0);
+    widen(0);
+    load_pages(min(k0 + KT, k1 - 1));
+  }
+  uint32_t stage = 0;
+  for (int k = k0; k < k1; k += KT) {
+    wait_all();
+    const bool more = k + KT < k1;
+    if (more) {
+      load(k + KT, STAGE - stage);
+      load_pages(min(k + 2 * KT, k1 - 1));
+    }
+    const bool here = live && k < hi_max && k + KT > lo_min, edge = k < lo_max || k + KT > hi_min;
+    if constexpr (BITS < 16) {
+      // rows whose value scale is NaN read as NaN
+      const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + stage + SOFF + 12 * KT);
+      if (uniform((int)(nan | nan >> 32)) != 0) {
+        for (int i = threadIdx.x; i < KT * LC; i += T)
+          if (nan >> (i / LC) & 1) *reinterpret_cast<u32x4 *>(smem + stage + VOFF + 16 * i) = u32x4{0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u};
+        wait_lds();
+      }
+    }
+    bool odd = false;            // a value is not finite, and not all rows see all keys
+    if (k < all_lo_max || k + KT > all_hi_min) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int i = 0; i < KT * LB / (16 * T); i++) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
+#pragma unroll
+        for (int j = 0; j < 4; j++) bad |= not_finite<VBF>(x[j]);
+      }
+      if (__any(bad != 0) && lane == 0) *flag = k / KT + 1;
+      wait_lds();
+      odd = uniform(*flag) == k / KT + 1;
+    }
+    if (!odd) {
+      if (here) {
+        scores(k, stage);
+        softmax(k, stage, edge);
+        products(stage + VOFF);
+      }
+    } else {
+      if (here) {
+        scores(k, stage);
+        softmax(k, stage, edge);
+      }
+      wait_lds();                // the keys have been read: their place takes ones where a value is not finite
+#pragma unroll
+      for (int i = 0; i < KT * LB / (16 * T); i++) {
+        u32x4 *const v = reinterpret_cast<u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
+        u32x4 x = *v, y;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const uint32_t b = (not_finite<VBF>(x[j]) >> 15) * 0xffffu;
+          y[j] = b & (kOne << 16 | kOne);
+          x[j] &= ~b;
+        }
+        *v = x;
+        *reinterpret_cast<u32x4 *>(smem + stage + 16 * (i * T + (int)threadIdx.x)) = y;
+      }
+      wait_lds();
+      if (here) {
+        products(stage + VOFF);
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+#pragma unroll
+          for (int t = 0; t < 2; t++)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+              pt[i][t][j] = (masked(k, i, 8 * t + 2 * j) ? 0u : kOne) | (masked(k, i, 8 * t + 2 * j + 1) ? 0u : kOne << 16);
+#pragma unroll
+        for (int c = 0; c < DT; c++) {
+          v16f n = {0};
+#pragma unroll
+          for (int i = 0; i < NK; i++)
+#pragma unroll
+            for (int t = 0; t < 2; t++) n = mfma32<VBF>(values_of(stage, i, t, c), pt[i][t], n);
+#pragma unroll
+          for (int v = 0; v < 16; v++) o[c][v] = n[v] > 0.0f ? NAN : o[c][v];
+        }
+      }
+    }
+    if (more) widen(STAGE - stage);
+    stage = STAGE - stage;
+  }
+
+  // ---- results
+  l += __shfl_xor(l, 32);
+  if (!live || row0 + 32 * w + r32 >= rows) return;
+  const int64_t to = (int64_t)(start + token) * a.hq + head;
+  if (a.splits == 1 && !a.shared) {
+    const float inv = 1.0f / l;
+    const bool none = l == 0.0f;
+#pragma unroll
+    for (int c = 0; c < DT; c++)
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) y[j] = none ? 0.0f : o[c][4 * g + j] * inv;
+        *reinterpret_cast<u32x2 *>(a.out + to * D + 32 * c + 8 * g + 4 * half) = u32x2{pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3])};
+      }
+    if (a.lse != nullptr && half == 0) a.lse[to] = none ? -INFINITY : log_sum(m, l);
+  } else {
+    const int64_t heads = (int64_t)a.tokens * a.hq, part = split * heads + to;
+    float *const op = a.scratch + 2 * a.splits * heads + part * D;
+#pragma unroll
+    for (int c = 0; c < DT; c++)
+#pragma unroll
+      for (int g = 0; g < 4; g++)
+        *reinterpret_cast<v4f *>(op + 32 * c + 8 * g + 4 * half) = v4f{o[c][4 * g], o[c][4 * g + 1], o[c][4 * g + 2], o[c][4 * g + 3]};
+    if (half == 0) *reinterpret_cast<f2 *>(a.scratch + 2 * part) = f2{m, l};
+  }
+}
+
+template <int D, int BITS, bool BF16, bool EXT>
+hipError_t go_prompt(const PromptArgs &a, hipStream_t s) {
+  const int bytes = prompt_lds_bytes(D, BITS);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(prompt_kernel<D, BITS, BF16, EXT>), bytes);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((prompt_kernel<D, BITS, BF16, EXT>), dim3((uint32_t)a.blocks), dim3(kPromptThreads), bytes, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// one head size's kernels (a file each)
+template <int D>
+hipError_t launch_prompt_d(const PromptArgs &a, bool bf16, hipStream_t s) {
+  const bool ext = a.cap > 0.0f || a.slopes != nullptr;
+  auto go = [&](auto bits, auto b) -> hipError_t {
+    return ext ? go_prompt<D, decltype(bits)::value, decltype(b)::value, true>(a, s)
+               : go_prompt<D, decltype(bits)::value, decltype(b)::value, false>(a, s);
+  };
+  auto go_type = [&](auto bits) -> hipError_t { return bf16 ? go(bits, std::true_type()) : go(bits, std::false_type()); };
+  if (a.c.bits == 16) return go_type(std::integral_constant<int, 16>());
+  if (a.c.bits == 8) return go_type(std::integral_constant<int, 8>());
+  return go_type(std::integral_constant<int, 4>());
+}
+
+}  // namespace tq

@@ -1,0 +1,8 @@
+// Attention of many tokens: the kernels for heads of 256 values.
+#include "tq_prompt.hpp"
+
+namespace tq {
+
+hipError_t launch_prompt_256(const PromptArgs &a, bool bf16, hipStream_t s) { return launch_prompt_d<256>(a, bf16, s); }
+
+}  // namespace tq

@@ -39,6 +39,8 @@ struct Entries {
   decltype(&tq_kv_read) read;
   decltype(&tq_paged_attention_scratch_bytes) scratch_bytes;
   decltype(&tq_paged_attention) attend;
+  decltype(&tq_prompt_attention_scratch_bytes) prompt_bytes;
+  decltype(&tq_prompt_attention) prompt;
 } L;
 PyObject *tq_error;         // TQError(code, where)
 PyObject *out_of_memory;    // torch's
@@ -368,6 +370,74 @@ PyObject *attend(PyObject *const *a, Py_ssize_t) {
   return return_lse ? wrap2(out, lse) : wrap(out);
 }
 
+// page_table [batch, max_pages] of strided rows: its address, and max_pages
+const int32_t *page_table_of(PyObject *o, const char *name, int64_t batch, int64_t dev, int &pages, int64_t &stride) {
+  const at::Tensor &t = tensor(o, name);
+  on_gpu(t, name, dev);
+  if (t.scalar_type() != at::kInt) bad_dtype(t, name, "Int");
+  if (t.dim() != 2 || t.size(0) != batch || t.size(1) == 0)
+    fail(PyExc_ValueError, "%s: shape %s, expected [%d, max_pages]", name, shape_of(t).c_str(), (int)batch);
+  pages = size32(t.size(1), name);
+  if ((t.stride(1) != 1 && pages > 1) || (t.stride(0) < pages && batch > 1)) fail(PyExc_ValueError, "%s: rows must be contiguous", name);
+  stride = t.stride(0);
+  return static_cast<const int32_t *>(t.data_ptr());
+}
+
+// scale or None, window, softcap, slopes or None: the scores of a call
+tq_scores scores_of(PyObject *scale, PyObject *window, PyObject *softcap, PyObject *slopes, int64_t hq, int64_t d, int64_t dev) {
+  tq_scores s = {};
+  s.scale = scale == Py_None ? (float)(1.0 / std::sqrt((double)d)) : (float)to_double(scale);
+  const int64_t win = window == nullptr ? 0 : to_int(window);
+  if (win < 0) fail(PyExc_ValueError, "window %lld: must not be negative", (long long)win);
+  s.window = win > INT32_MAX ? 0 : (int32_t)win;      // (past any length: none)
+  s.softcap = (float)to_double(softcap);
+  if (!(s.softcap >= 0.0f) || std::isinf(s.softcap)) fail(PyExc_ValueError, "softcap: must be finite and not negative (0: none)");
+  s.slopes = static_cast<const float *>(plain_or_null(slopes, "slopes", at::kFloat, {hq}, dev));
+  return s;
+}
+
+// query rows next to a cache: tokens (or -1), and their heads, a multiple of the cache's
+const at::Tensor &queries(PyObject *o, const Cache &c, int64_t dev, tq_head_rows &q) {
+  const at::Tensor &t = rows(o, "q", dev, -1, -1, c.c.head_dim, q);
+  cache_type(c, t, "q");
+  if (t.size(1) == 0 || t.size(1) % c.c.kv_heads != 0)
+    fail(PyExc_ValueError, "q: %d heads are no multiple of the cache's %d", (int)t.size(1), c.c.kv_heads);
+  return t;
+}
+
+// prompt(cache, q, starts, page_table, lengths, scale or None, window, prefix or None, first or None, softcap,
+//        slopes or None, return_lse, device, stream): out or (out, lse)
+PyObject *prompt(PyObject *const *a, Py_ssize_t) {
+  const int64_t dev = to_int(a[12]);
+  const Cache &c = cache_of(a[0], dev);
+  tq_head_rows q;
+  const at::Tensor &qt = queries(a[1], c, dev, q);
+  const int tokens = size32(qt.size(0), "q"), hq = size32(qt.size(1), "q");
+  const at::Tensor &st = tensor(a[2], "starts");
+  if (st.dim() != 1 || st.size(0) < 2) fail(PyExc_ValueError, "starts: shape %s, expected (batch + 1) with a batch of at least 1", shape_of(st).c_str());
+  const int batch = size32(st.size(0) - 1, "starts");
+  const int32_t *starts = static_cast<const int32_t *>(plain(a[2], "starts", at::kInt, {batch + 1}, dev));
+  int pages;
+  int64_t stride;
+  const int32_t *table = page_table_of(a[3], "page_table", batch, dev, pages, stride);
+  const int32_t *lengths = static_cast<const int32_t *>(plain(a[4], "lengths", at::kInt, {batch}, dev));
+  const int32_t *prefix = static_cast<const int32_t *>(plain_or_null(a[7], "prefix", at::kInt, {batch}, dev));
+  const int32_t *first = static_cast<const int32_t *>(plain_or_null(a[8], "first", at::kInt, {tokens}, dev));
+  const tq_scores s = scores_of(a[5], a[6], a[9], a[10], hq, c.c.head_dim, dev);
+  const bool return_lse = to_bool(a[11]);
+  const size_t bytes = L.prompt_bytes(&c.c, tokens, batch, hq, pages, s.window);
+  const at::Tensor out = fresh({tokens, hq, c.c.head_dim}, qt.scalar_type(), dev);
+  at::Tensor lse, scratch;
+  if (return_lse) lse = fresh({tokens, hq}, at::kFloat, dev);
+  if (bytes > 0) scratch = fresh({(int64_t)(bytes / 4)}, at::kFloat, dev);
+  if (tokens > 0)
+    check(L.prompt(&c.c, &q, dtype_of(qt.scalar_type()), tokens, batch, hq, starts, table, stride, pages, lengths, prefix, first,
+                   &s, out.data_ptr(), return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr,
+                   bytes > 0 ? scratch.data_ptr() : nullptr, to_stream(a[13])),
+          "tq_prompt_attention");
+  return return_lse ? wrap2(out, lse) : wrap(out);
+}
+
 // bind(TQError, torch.OutOfMemoryError, addresses of the entry points, in the order of Entries)
 PyObject *bind(PyObject *const *a, Py_ssize_t) {
   Py_INCREF(a[0]);
@@ -381,6 +451,8 @@ PyObject *bind(PyObject *const *a, Py_ssize_t) {
   L.read = reinterpret_cast<decltype(L.read)>(to_stream(a[4]));
   L.scratch_bytes = reinterpret_cast<decltype(L.scratch_bytes)>(to_stream(a[5]));
   L.attend = reinterpret_cast<decltype(L.attend)>(to_stream(a[6]));
+  L.prompt_bytes = reinterpret_cast<decltype(L.prompt_bytes)>(to_stream(a[7]));
+  L.prompt = reinterpret_cast<decltype(L.prompt)>(to_stream(a[8]));
   Py_RETURN_NONE;
 }
 
@@ -408,8 +480,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define TQ_METHOD(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TQ_METHOD(bind, 8), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
-                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 9),
+PyMethodDef methods[] = {TQ_METHOD(bind, 10), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
+                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 9), TQ_METHOD(prompt, 14),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

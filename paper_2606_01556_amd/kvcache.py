@@ -25,7 +25,7 @@ import os
 from . import TQError, _HERE, _other_stream, _stream, lib
 
 __all__ = ["KVCache", "empty_kv_cache", "rope_table", "kv_append", "kv_read", "qk_norm_rope",
-           "qk_norm_rope_append", "paged_attention"]
+           "qk_norm_rope_append", "paged_attention", "prompt_attention"]
 
 
 class _CacheDesc(ctypes.Structure):     # tq_kv_cache
@@ -45,6 +45,11 @@ class _NormRope(ctypes.Structure):      # tq_norm_rope
                 ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class _Scores(ctypes.Structure):        # tq_scores
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p),
+                ("window", ctypes.c_int32)]
+
+
 def declare(L):
     """Argument types of this module's entry points (called as the library loads)."""
     P, I = ctypes.c_void_p, ctypes.c_int
@@ -56,6 +61,10 @@ def declare(L):
     L.tq_paged_attention_scratch_bytes.argtypes = [C, I, I, I, I]
     L.tq_paged_attention_scratch_bytes.restype = ctypes.c_size_t
     L.tq_paged_attention.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, ctypes.c_float, I, P, P, P, P]
+    S = ctypes.POINTER(_Scores)
+    L.tq_prompt_attention_scratch_bytes.argtypes = [C, I, I, I, I, I]
+    L.tq_prompt_attention_scratch_bytes.restype = ctypes.c_size_t
+    L.tq_prompt_attention.argtypes = [C, H, I, I, I, I, P, P, ctypes.c_int64, I, P, P, P, S, P, P, P, P]
 
 
 # ------------------------------------------------------------------ the native half
@@ -76,7 +85,8 @@ def _load():
     L = lib()
     native.bind(TQError, torch.OutOfMemoryError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.tq_qk_norm_rope, L.tq_kv_append, L.tq_qk_norm_rope_append, L.tq_kv_read,
-        L.tq_paged_attention_scratch_bytes, L.tq_paged_attention)))
+        L.tq_paged_attention_scratch_bytes, L.tq_paged_attention, L.tq_prompt_attention_scratch_bytes,
+        L.tq_prompt_attention)))
     _torch, _get_device, _get_raw = torch, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _native = native
     return native
@@ -245,3 +255,29 @@ def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None 
         return _elsewhere(stream, (q, page_table, lengths, *cache._t), lambda dev, st: _native.attend(
             c, q, page_table, lengths, scale, window, return_lse, dev, st))
     return _native.attend(c, q, page_table, lengths, scale, window, return_lse, *_here())
+
+
+def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: float | None = None, window: int = 0,
+                     prefix=None, first=None, softcap: float = 0.0, slopes=None, return_lse: bool = False, stream=None):
+    """Attention of many new tokens of every stream over the cache, which holds them
+    already (tq_prompt_attention): prompts, chunks of prompts, tokens to verify.  q
+    [tokens, q_heads, head_dim] holds the streams' new tokens one stream after the other,
+    stream i's in rows starts[i] to starts[i + 1] (starts [batch + 1] int32); they are the
+    last of its lengths[i] tokens.  page_table and lengths as in ``paged_attention``.
+
+    A token sees itself and what is before it, with window > 0 only the last so many;
+    with prefix [batch] int32 also all of its stream's first prefix[i] tokens; with first
+    [tokens] int32 nothing before position first[r] (where its document starts).  softcap
+    > 0: scores s become softcap * tanh(s / softcap); slopes [q_heads] float32: less
+    slopes[h] times the distance.  scale: head_dim^-1/2 by default.
+
+    Returns out [tokens, q_heads, head_dim] of q's type, zeros for a token that sees
+    nothing and for rows of no stream; with return_lse (out, lse [tokens, q_heads]
+    float32)."""
+    c = _handle(cache)
+    if stream is not None:
+        return _elsewhere(stream, (q, starts, page_table, lengths, prefix, first, slopes, *cache._t),
+                          lambda dev, st: _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first,
+                                                         softcap, slopes, return_lse, dev, st))
+    return _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first, softcap, slopes, return_lse,
+                          *_here())
