@@ -433,6 +433,15 @@ typedef struct {
     int32_t window;
 } tq_scores;
 
+/* tq_paged_attention with such scores, the token at position lengths[i] - 1 (its scratch
+ * size is tq_paged_attention_scratch_bytes).  With softcap 0 and no slopes it is
+ * tq_paged_attention.  The tanh is good to 2^-22 of the cap.
+ * Errors as tq_paged_attention; TQ_ERR_SHAPE for a softcap that is negative or not finite. */
+tq_status tq_paged_attention_scored(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
+                                    int q_heads, const int32_t *page_table, int64_t table_stride,
+                                    int max_pages, const int32_t *lengths, const tq_scores *scores, void *out,
+                                    float *lse, void *scratch, void *stream);
+
 /* Attention of many new tokens of every stream over the cache, which holds them already
  * (prompts, chunks of prompts, tokens to verify):
  *   out[r, h] = sum_j w_j v_j,  w = softmax over j of the scores
@@ -468,6 +477,36 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
                               int64_t table_stride, int max_pages, const int32_t *lengths,
                               const int32_t *prefix, const int32_t *first, const tq_scores *scores, void *out,
                               float *lse, void *scratch, void *stream);
+
+/* Attention of one new token of every stream over a prefix that a group of streams shares and
+ * over the stream's own tokens behind it; the prefix is read once for all of its group:
+ *   out[i, h] = sum_j w_j v_j,  w = softmax of the scores over the prefix's and the stream's keys
+ *   q               [batch, q_heads, head_dim] of type dtype
+ *   members         [groups + 1] int32: group g's streams are members[g] .. members[g + 1] - 1
+ *                   (ascending, taken into [0, batch]); a stream of no group has no prefix
+ *   prefix_table    [groups] rows of prefix_pages page numbers, prefix_stride apart: the
+ *                   pages of a group's prefix
+ *   prefix_lengths  [groups] int32, taken into [0, prefix_pages * page_size]
+ *   page_table, table_stride, max_pages, lengths  of the streams' own tokens, as in
+ *                   tq_paged_attention.  Stream i's new token has the position (prefix length +
+ *                   lengths[i] - 1), its own token j the position (prefix length + j)
+ *   scores          window has to be 0
+ *   lse             [batch, q_heads] fp32 or NULL
+ *   scratch         device buffer of tq_shared_prefix_attention_scratch_bytes bytes (never 0 for a
+ *                   batch), 16-byte aligned, free again when the stream has run the call
+ * A stream without prefix and tokens gives zeros and -infinity.  Precision as in
+ * tq_prompt_attention for the prefix's keys, as in tq_paged_attention for a stream's own.
+ * Three launches; the result does not depend on timing.  batch == 0 is a no-op; groups from 1
+ * to 65535, batch and both tables within the limits of the two.
+ * Errors as tq_prompt_attention. */
+size_t tq_shared_prefix_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int groups,
+                                                int prefix_pages, int max_pages);
+tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
+                                     int q_heads, int groups, const int32_t *members,
+                                     const int32_t *prefix_table, int64_t prefix_stride, int prefix_pages,
+                                     const int32_t *prefix_lengths, const int32_t *page_table,
+                                     int64_t table_stride, int max_pages, const int32_t *lengths,
+                                     const tq_scores *scores, void *out, float *lse, void *scratch, void *stream);
 
 /* Static description of a status code; never NULL. */
 const char *tq_status_string(tq_status s);

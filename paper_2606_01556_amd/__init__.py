@@ -48,7 +48,8 @@ EXPORTS = ("tq_weight_desc_init", "tq_pack_weights", "tq_quant_act", "tq_dual_ge
            "tq_dual_gemm_unfused_noalloc", "tq_dual_gemm_kernel", "tq_dual_gemm_block", "tq_status_string",
            "tq_export_weights_canonical", "tq_act_codes_canonical", "tq_layer",
            "tq_layer_scratch_bytes", "tq_qk_norm_rope", "tq_kv_append", "tq_qk_norm_rope_append", "tq_kv_read",
-           "tq_paged_attention_scratch_bytes", "tq_paged_attention", "tq_prompt_attention_scratch_bytes", "tq_prompt_attention")
+           "tq_paged_attention_scratch_bytes", "tq_paged_attention", "tq_prompt_attention_scratch_bytes", "tq_prompt_attention",
+           "tq_paged_attention_scored", "tq_shared_prefix_attention_scratch_bytes", "tq_shared_prefix_attention")
 
 _lib = None
 
@@ -88,7 +89,8 @@ def lib() -> ctypes.CDLL:
         L.tq_status_string.restype = ctypes.c_char_p
         kvcache.declare(L)
         for name in EXPORTS:
-            if name not in ("tq_act_codes_bytes", "tq_paged_attention_scratch_bytes", "tq_prompt_attention_scratch_bytes", "tq_unfused_scratch_bytes", "tq_layer_scratch_bytes",
+            if name not in ("tq_act_codes_bytes", "tq_paged_attention_scratch_bytes", "tq_prompt_attention_scratch_bytes",
+                            "tq_shared_prefix_attention_scratch_bytes", "tq_unfused_scratch_bytes", "tq_layer_scratch_bytes",
                             "tq_dual_gemm_kernel", "tq_status_string"):
                 getattr(L, name).restype = I
         _lib = L
@@ -538,4 +540,4 @@ def act_codes_rows(x_codes, m: int) -> np.ndarray:
 
 from . import kvcache                                                          # noqa: E402
 from .kvcache import (KVCache, empty_kv_cache, kv_append, kv_read, paged_attention,   # noqa: E402,F401
-                      prompt_attention, qk_norm_rope, qk_norm_rope_append, rope_table)
+                      prompt_attention, qk_norm_rope, qk_norm_rope_append, rope_table, shared_prefix_attention)

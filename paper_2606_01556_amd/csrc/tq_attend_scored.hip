@@ -1,0 +1,9 @@
+// Attention of one new token per stream with capped or biased scores, or with its parts as
+// the result: the kernels.  (32 streams up to 8192 tokens, 8 bits, a cap: see tq_attend.hpp.)
+#include "tq_attend.hpp"
+
+namespace tq {
+
+hipError_t launch_attend_scored(const AttendArgs &a, bool bf16, hipStream_t s) { return go_heads<true>(a, bf16, s); }
+
+}  // namespace tq

@@ -46,6 +46,18 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// Scores under a cap, in binades: cap tanh x = cap (1 - 2 / (e^2x + 1)), good to 2^-22 of the
+// cap.  `in` turns a product of a query and a key into the exponent, log2(e) 2 x.
+struct Shape {
+  float in, out;
+};
+__device__ __forceinline__ Shape shape_of(float scale, float cap, float unit) {
+  return {cap > 0.0f ? 2.0f * kLog2e * (fabsf(scale) / cap) * unit : 0.0f, cap * kLog2e};
+}
+__device__ __forceinline__ float capped(float product, const Shape &s) {
+  return fmaf(__builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(product * s.in) + 1.0f), -2.0f * s.out, s.out);
+}
+
 // log-sum-exp in natural units from the reference m and the sum l of exp2(score - m)
 // (m and l's binade all but cancel: they go together first)
 __device__ __forceinline__ float log_sum(float m, float l) {

@@ -66,6 +66,9 @@ struct AttendArgs {
   float *scratch;
   int blocks;                // work-groups
   int direct;
+  float cap;                 // 0: none
+  const float *slopes;       // [hq] or null
+  bool parts;                // the parts in scratch are the result: no join, nothing written to out
 };
 
 // Attention of many new tokens of every stream, or (shared) of the streams of every group over
@@ -81,7 +84,8 @@ struct PromptArgs {
   int64_t table_stride;
   int max_pages;
   const int32_t *lengths;    // [batch]
-  const int32_t *own;        // shared: [tokens] tokens behind the prefix
+  const int32_t *own;        // shared: [tokens] tokens behind the prefix, taken into [0, own_most]
+  int own_most;
   const int32_t *prefix, *first;   // [batch], [tokens], or null
   float scale, cap;          // cap 0: none
   const float *slopes;       // [hq] or null
@@ -95,6 +99,9 @@ struct PromptArgs {
   int64_t blocks;
 };
 
+// floats of the references and sums in front of the products (which start on 16 bytes)
+__host__ __device__ inline int64_t parts_head(int splits, int64_t heads) { return (2 * splits * heads + 3) & ~(int64_t)3; }
+
 hipError_t launch_tokens(const TokenArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_kv_read(const ReadArgs &a, bool bf16, hipStream_t s);
 // How an attention call is cut, by what the host knows of it: direct, one
@@ -107,6 +114,7 @@ struct AttendPlan {
 };
 AttendPlan attend_plan(const KvCache &c, int batch, int hq, int64_t max_len, int window);
 hipError_t launch_attend(const AttendArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_attend_scored(const AttendArgs &a, bool bf16, hipStream_t s);
 
 // How an attention of many tokens is cut: row tiles (a bound over all streams) and parts of
 // a tile's keys.
@@ -117,6 +125,14 @@ struct PromptPlan {
 };
 PromptPlan prompt_plan(const KvCache &c, int tokens, int batch, int hq, int64_t max_len, int window, bool shared);
 hipError_t launch_prompt(const PromptArgs &a, bool bf16, hipStream_t s);
+// Attention of one token of every stream over a shared prefix and its own tokens: both leave parts.
+struct PrefixArgs {
+  PromptArgs prefix;         // shared; its tokens are the streams, its streams the groups
+  AttendArgs own;            // parts
+};
+// bytes of the parts that launch_attend leaves
+size_t attend_parts_bytes(const KvCache &c, int batch, int hq, const AttendPlan &p);
+hipError_t launch_prefix(const PrefixArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_prompt_64(const PromptArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_prompt_128(const PromptArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_prompt_256(const PromptArgs &a, bool bf16, hipStream_t s);

@@ -183,18 +183,26 @@ size_t tq_paged_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_h
   return p.scratch;
 }
 
-tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
-                             int q_heads, const int32_t *page_table, int64_t table_stride, int max_pages,
-                             const int32_t *lengths, float scale, int window, void *out, float *lse,
-                             void *scratch, void *stream) {
+// the scores of a call
+static tq_status check_scores(const tq_scores *s) {
+  if (s == nullptr) return TQ_ERR_NULL;
+  if (!std::isfinite(s->scale) || !std::isfinite(s->softcap) || s->softcap < 0.0f || s->window < 0) return TQ_ERR_SHAPE;
+  if (!aligned(s->slopes, 4)) return TQ_ERR_ALIGN;
+  return TQ_OK;
+}
+
+static tq_status attend(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch, int q_heads,
+                        const int32_t *page_table, int64_t table_stride, int max_pages, const int32_t *lengths,
+                        const tq_scores *scores, void *out, float *lse, void *scratch, void *stream) {
   tq::AttendArgs a = {};
   if (page_table == nullptr || lengths == nullptr || out == nullptr) return TQ_ERR_NULL;
   TQ_TRY(check_cache(c, a.c));
   tq::HeadRows rows;
   TQ_TRY(check_rows(q, rows));
+  TQ_TRY(check_scores(scores));
   tq::AttendPlan p;
-  TQ_TRY(attention_plan(c, a.c, batch, q_heads, max_pages, window, p));
-  if (table_stride < 0 || !std::isfinite(scale)) return TQ_ERR_SHAPE;
+  TQ_TRY(attention_plan(c, a.c, batch, q_heads, max_pages, scores->window, p));
+  if (table_stride < 0) return TQ_ERR_SHAPE;
   if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
   if (!aligned(page_table, 4) || !aligned(lengths, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(scratch))
     return TQ_ERR_ALIGN;
@@ -204,7 +212,7 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
   a.batch = batch; a.hq = q_heads; a.group = q_heads / c->kv_heads;
   a.table = page_table; a.table_stride = table_stride; a.max_pages = max_pages;
   a.lengths = lengths;
-  a.scale = scale; a.window = window;
+  a.scale = scores->scale; a.window = scores->window; a.cap = scores->softcap; a.slopes = scores->slopes;
   a.out = static_cast<uint16_t *>(out);
   a.lse = lse;
   a.scratch = static_cast<float *>(scratch);
@@ -213,12 +221,18 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
   return hip_status(tq::launch_attend(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
-// the scores of a call
-static tq_status check_scores(const tq_scores *s) {
-  if (s == nullptr) return TQ_ERR_NULL;
-  if (!std::isfinite(s->scale) || !std::isfinite(s->softcap) || s->softcap < 0.0f || s->window < 0) return TQ_ERR_SHAPE;
-  if (!aligned(s->slopes, 4)) return TQ_ERR_ALIGN;
-  return TQ_OK;
+tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
+                             int q_heads, const int32_t *page_table, int64_t table_stride, int max_pages,
+                             const int32_t *lengths, float scale, int window, void *out, float *lse,
+                             void *scratch, void *stream) {
+  const tq_scores scores = {scale, 0.0f, nullptr, window};
+  return attend(c, q, dtype, batch, q_heads, page_table, table_stride, max_pages, lengths, &scores, out, lse, scratch, stream);
+}
+
+tq_status tq_paged_attention_scored(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch, int q_heads,
+                                    const int32_t *page_table, int64_t table_stride, int max_pages, const int32_t *lengths,
+                                    const tq_scores *scores, void *out, float *lse, void *scratch, void *stream) {
+  return attend(c, q, dtype, batch, q_heads, page_table, table_stride, max_pages, lengths, scores, out, lse, scratch, stream);
 }
 
 static tq_status plan_prompt(const tq_kv_cache *c, const tq::KvCache &k, int tokens, int batch, int q_heads, int max_pages,
@@ -269,6 +283,80 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
   a.scratch = static_cast<float *>(scratch);
   a.tiles = p.tiles; a.splits = p.splits; a.blocks = p.blocks;
   return hip_status(tq::launch_prompt(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
+}
+
+// both halves of a call, and where the second one's parts begin in scratch
+static tq_status plan_prefix(const tq_kv_cache *c, const tq::KvCache &k, int batch, int q_heads, int groups, int prefix_pages,
+                             int max_pages, tq::PromptPlan &p, tq::AttendPlan &t, size_t &first, size_t &bytes) {
+  if (groups < 1 || groups > 65535 || batch < 0) return TQ_ERR_SHAPE;
+  TQ_TRY(attention_plan(c, k, batch, q_heads, max_pages, 0, t));
+  TQ_TRY(plan_prompt(c, k, batch, groups, q_heads, prefix_pages, 0, true, p));
+  first = (p.scratch + 255) & ~(size_t)255;
+  bytes = batch == 0 ? 0 : first + tq::attend_parts_bytes(k, batch, q_heads, t);
+  return TQ_OK;
+}
+
+size_t tq_shared_prefix_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int groups, int prefix_pages,
+                                                int max_pages) {
+  tq::KvCache k;
+  tq::PromptPlan p;
+  tq::AttendPlan t;
+  size_t first, bytes;
+  if (check_cache(c, k) != TQ_OK || plan_prefix(c, k, batch, q_heads, groups, prefix_pages, max_pages, p, t, first, bytes) != TQ_OK)
+    return 0;
+  return bytes;
+}
+
+tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch, int q_heads,
+                                     int groups, const int32_t *members, const int32_t *prefix_table, int64_t prefix_stride,
+                                     int prefix_pages, const int32_t *prefix_lengths, const int32_t *page_table,
+                                     int64_t table_stride, int max_pages, const int32_t *lengths, const tq_scores *scores,
+                                     void *out, float *lse, void *scratch, void *stream) {
+  tq::PrefixArgs a = {};
+  if (members == nullptr || prefix_table == nullptr || prefix_lengths == nullptr || page_table == nullptr ||
+      lengths == nullptr || out == nullptr)
+    return TQ_ERR_NULL;
+  tq::KvCache k;
+  TQ_TRY(check_cache(c, k));
+  tq::HeadRows rows;
+  TQ_TRY(check_rows(q, rows));
+  TQ_TRY(check_scores(scores));
+  tq::PromptPlan p;
+  tq::AttendPlan t;
+  size_t first, bytes;
+  TQ_TRY(plan_prefix(c, k, batch, q_heads, groups, prefix_pages, max_pages, p, t, first, bytes));
+  if (prefix_stride < 0 || table_stride < 0 || scores->window != 0) return TQ_ERR_SHAPE;
+  if (!dtype_ok(dtype) || (c->bits == 16 && dtype != c->dtype)) return TQ_ERR_DTYPE;
+  if (!aligned(members, 4) || !aligned(prefix_table, 4) || !aligned(prefix_lengths, 4) || !aligned(page_table, 4) ||
+      !aligned(lengths, 4) || !aligned16(out) || !aligned(lse, 4) || !aligned16(scratch))
+    return TQ_ERR_ALIGN;
+  if (batch == 0) return TQ_OK;
+  if (scratch == nullptr) return TQ_ERR_NULL;
+  tq::PromptArgs &x = a.prefix;
+  x.c = k;
+  x.q = rows.p; x.q_ts = rows.ts; x.q_hs = rows.hs;
+  x.tokens = batch; x.hq = q_heads; x.group = q_heads / c->kv_heads; x.batch = groups;
+  x.starts = members;
+  x.table = prefix_table; x.table_stride = prefix_stride; x.max_pages = prefix_pages;
+  x.lengths = prefix_lengths; x.own = lengths; x.own_most = max_pages * c->page_size;
+  x.scale = scores->scale; x.cap = scores->softcap; x.slopes = scores->slopes;
+  x.shared = true;
+  x.out = static_cast<uint16_t *>(out);
+  x.lse = lse;
+  x.scratch = static_cast<float *>(scratch);
+  x.tiles = p.tiles; x.splits = p.splits; x.blocks = p.blocks;
+  tq::AttendArgs &y = a.own;
+  y.c = k;
+  y.q = rows.p; y.q_ts = rows.ts; y.q_hs = rows.hs;
+  y.batch = batch; y.hq = q_heads; y.group = x.group;
+  y.table = page_table; y.table_stride = table_stride; y.max_pages = max_pages;
+  y.lengths = lengths;
+  y.scale = x.scale; y.cap = x.cap; y.slopes = x.slopes;
+  y.parts = true;
+  y.scratch = reinterpret_cast<float *>(static_cast<uint8_t *>(scratch) + first);
+  y.direct = t.direct;
+  y.blocks = t.blocks;
+  return hip_status(tq::launch_prefix(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

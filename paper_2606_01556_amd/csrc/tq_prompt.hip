@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const PromptArg
     for (int i = 0; i < 4; i++) o[i] = o[i] * f0 + y[i] * f1;
   };
   if (live) {
-    const float *const parts = a.scratch + 2 * a.splits * heads;
+    const float *const parts = a.scratch + parts_head(a.splits, heads);
 #pragma unroll 4
     for (int k = mine; k < a.splits; k += side)
       add(*reinterpret_cast<const f2 *>(a.scratch + 2 * (k * heads + row)), *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
@@ -78,7 +78,7 @@ PromptPlan prompt_plan(const KvCache &c, int tokens, int batch, int hq, int64_t 
   p.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
   p.splits = (int)splits;
   p.blocks = units * splits;
-  p.scratch = splits > 1 || shared ? (size_t)splits * tokens * hq * (2 + c.d) * sizeof(float) : 0;
+  p.scratch = splits > 1 || shared ? (size_t)(parts_head(p.splits, (int64_t)tokens * hq) + splits * tokens * hq * c.d) * sizeof(float) : 0;
   return p;
 }
 

@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   int pos;
   Interval seen;
   if (a.shared) {
-    const int own = min(max(a.own[start + token], 0), 1 << 30);
+    const int own = min(max(a.own[start + token], 0), a.own_most);
     pos = len + own - 1;
     seen = {0, len};
   } else {
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
 
   // what a score's product with the key's scale is multiplied by, in binades
   const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f);     // (-infinity times it has to stay so)
-  const float cap_in = EXT && a.cap > 0.0f ? 2.0f * kLog2e * (fabsf(a.scale) / a.cap) : 0.0f, cap_out = a.cap * kLog2e;
+  const Shape shape = EXT ? shape_of(a.scale, a.cap, 1.0f) : Shape{};
   const float slope = EXT && a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.0f;
   // binades above the reference at which it has to move, and where it puts the largest weight
   float most = kTopBinades, headroom = kHeadroom;
@@ -337,14 +337,10 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
     }
     if constexpr (EXT) {
       if (a.cap > 0.0f) {
-        // cap tanh x = cap (1 - 2 / (e^2x + 1)), good to 2^-23 of the cap
 #pragma unroll
         for (int i = 0; i < NK; i++)
 #pragma unroll
-          for (int v = 0; v < 16; v++) {
-            const float e = __builtin_amdgcn_exp2f(sc[i][v] * cap_in);
-            sc[i][v] = fmaf(__builtin_amdgcn_rcpf(e + 1.0f), -2.0f * cap_out, cap_out);
-          }
+          for (int v = 0; v < 16; v++) sc[i][v] = capped(sc[i][v], shape);
       } else {
 #pragma unroll
         for (int i = 0; i < NK; i++)
@@ -549,7 +545,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
     if (a.lse != nullptr && half == 0) a.lse[to] = none ? -INFINITY : log_sum(m, l);
   } else {
     const int64_t heads = (int64_t)a.tokens * a.hq, part = split * heads + to;
-    float *const op = a.scratch + 2 * a.splits * heads + part * D;
+    float *const op = a.scratch + parts_head(a.splits, heads) + part * D;
 #pragma unroll
     for (int c = 0; c < DT; c++)
 #pragma unroll

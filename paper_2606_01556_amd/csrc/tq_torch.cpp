@@ -38,9 +38,11 @@ struct Entries {
   decltype(&tq_qk_norm_rope_append) norm_rope_append;
   decltype(&tq_kv_read) read;
   decltype(&tq_paged_attention_scratch_bytes) scratch_bytes;
-  decltype(&tq_paged_attention) attend;
   decltype(&tq_prompt_attention_scratch_bytes) prompt_bytes;
   decltype(&tq_prompt_attention) prompt;
+  decltype(&tq_paged_attention_scored) attend_scored;
+  decltype(&tq_shared_prefix_attention_scratch_bytes) prefix_bytes;
+  decltype(&tq_shared_prefix_attention) prefix;
 } L;
 PyObject *tq_error;         // TQError(code, where)
 PyObject *out_of_memory;    // torch's
@@ -332,44 +334,6 @@ PyObject *norm_rope_append(PyObject *const *a, Py_ssize_t) {
   return return_k ? wrap2(qo, ko) : wrap(qo);
 }
 
-// attend(cache, q, page_table, lengths, scale or None, window, return_lse, device, stream): out or (out, lse)
-PyObject *attend(PyObject *const *a, Py_ssize_t) {
-  const int64_t dev = to_int(a[7]);
-  const Cache &c = cache_of(a[0], dev);
-  const int64_t d = c.c.head_dim;
-  tq_head_rows q;
-  const at::Tensor &qt = rows(a[1], "q", dev, -1, -1, d, q);
-  cache_type(c, qt, "q");
-  const int batch = size32(qt.size(0), "q"), hq = size32(qt.size(1), "q");
-  if (hq == 0 || hq % c.c.kv_heads != 0)
-    fail(PyExc_ValueError, "q: %d heads are no multiple of the cache's %d", hq, c.c.kv_heads);
-  const at::Tensor &pt = tensor(a[2], "page_table");
-  on_gpu(pt, "page_table", dev);
-  if (pt.scalar_type() != at::kInt) bad_dtype(pt, "page_table", "Int");
-  if (pt.dim() != 2 || pt.size(0) != batch || pt.size(1) == 0)
-    fail(PyExc_ValueError, "page_table: shape %s, expected [%d, max_pages]", shape_of(pt).c_str(), batch);
-  const int pages = size32(pt.size(1), "page_table");
-  if ((pt.stride(1) != 1 && pages > 1) || (pt.stride(0) < pages && batch > 1))
-    fail(PyExc_ValueError, "page_table: rows must be contiguous");
-  const int32_t *lengths = static_cast<const int32_t *>(plain(a[3], "lengths", at::kInt, {batch}, dev));
-  const float scale = a[4] == Py_None ? (float)(1.0 / std::sqrt((double)d)) : (float)to_double(a[4]);
-  const int64_t window = to_int(a[5]);
-  if (window < 0) fail(PyExc_ValueError, "window %lld: must not be negative", (long long)window);
-  const int win = window > INT32_MAX ? 0 : (int)window;      // (past any length: none)
-  const bool return_lse = to_bool(a[6]);
-  const size_t bytes = L.scratch_bytes(&c.c, batch, hq, pages, win);
-  const at::Tensor out = fresh({batch, hq, d}, qt.scalar_type(), dev);
-  at::Tensor lse, scratch;
-  if (return_lse) lse = fresh({batch, hq}, at::kFloat, dev);
-  if (bytes > 0) scratch = fresh({(int64_t)(bytes / 4)}, at::kFloat, dev);
-  if (batch > 0)
-    check(L.attend(&c.c, &q, dtype_of(qt.scalar_type()), batch, hq, static_cast<const int32_t *>(pt.data_ptr()), pt.stride(0),
-                   pages, lengths, scale, win, out.data_ptr(), return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr,
-                   bytes > 0 ? scratch.data_ptr() : nullptr, to_stream(a[8])),
-          "tq_paged_attention");
-  return return_lse ? wrap2(out, lse) : wrap(out);
-}
-
 // page_table [batch, max_pages] of strided rows: its address, and max_pages
 const int32_t *page_table_of(PyObject *o, const char *name, int64_t batch, int64_t dev, int &pages, int64_t &stride) {
   const at::Tensor &t = tensor(o, name);
@@ -403,6 +367,67 @@ const at::Tensor &queries(PyObject *o, const Cache &c, int64_t dev, tq_head_rows
   if (t.size(1) == 0 || t.size(1) % c.c.kv_heads != 0)
     fail(PyExc_ValueError, "q: %d heads are no multiple of the cache's %d", (int)t.size(1), c.c.kv_heads);
   return t;
+}
+
+// attend(cache, q, page_table, lengths, scale or None, window, return_lse, softcap, slopes or None, device, stream):
+// out or (out, lse)
+PyObject *attend(PyObject *const *a, Py_ssize_t) {
+  const int64_t dev = to_int(a[9]);
+  const Cache &c = cache_of(a[0], dev);
+  tq_head_rows q;
+  const at::Tensor &qt = queries(a[1], c, dev, q);
+  const int batch = size32(qt.size(0), "q"), hq = size32(qt.size(1), "q");
+  int pages;
+  int64_t stride;
+  const int32_t *table = page_table_of(a[2], "page_table", batch, dev, pages, stride);
+  const int32_t *lengths = static_cast<const int32_t *>(plain(a[3], "lengths", at::kInt, {batch}, dev));
+  const tq_scores s = scores_of(a[4], a[5], a[7], a[8], hq, c.c.head_dim, dev);
+  const bool return_lse = to_bool(a[6]);
+  const size_t bytes = L.scratch_bytes(&c.c, batch, hq, pages, s.window);
+  const at::Tensor out = fresh({batch, hq, c.c.head_dim}, qt.scalar_type(), dev);
+  at::Tensor lse, scratch;
+  if (return_lse) lse = fresh({batch, hq}, at::kFloat, dev);
+  if (bytes > 0) scratch = fresh({(int64_t)(bytes / 4)}, at::kFloat, dev);
+  if (batch > 0)
+    check(L.attend_scored(&c.c, &q, dtype_of(qt.scalar_type()), batch, hq, table, stride, pages, lengths, &s, out.data_ptr(),
+                          return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, bytes > 0 ? scratch.data_ptr() : nullptr,
+                          to_stream(a[10])),
+          "tq_paged_attention");
+  return return_lse ? wrap2(out, lse) : wrap(out);
+}
+
+// prefix(cache, q, members, prefix_table, prefix_lengths, page_table, lengths, scale or None, softcap, slopes or None,
+//        return_lse, device, stream): out or (out, lse)
+PyObject *prefix(PyObject *const *a, Py_ssize_t) {
+  const int64_t dev = to_int(a[11]);
+  const Cache &c = cache_of(a[0], dev);
+  tq_head_rows q;
+  const at::Tensor &qt = queries(a[1], c, dev, q);
+  const int batch = size32(qt.size(0), "q"), hq = size32(qt.size(1), "q");
+  const at::Tensor &mt = tensor(a[2], "members");
+  if (mt.dim() != 1 || mt.size(0) < 2) fail(PyExc_ValueError, "members: shape %s, expected (groups + 1) with at least 1 group", shape_of(mt).c_str());
+  const int groups = size32(mt.size(0) - 1, "members");
+  const int32_t *members = static_cast<const int32_t *>(plain(a[2], "members", at::kInt, {groups + 1}, dev));
+  int prefix_pages, pages;
+  int64_t prefix_stride, stride;
+  const int32_t *prefix_table = page_table_of(a[3], "prefix_table", groups, dev, prefix_pages, prefix_stride);
+  const int32_t *prefix_lengths = static_cast<const int32_t *>(plain(a[4], "prefix_lengths", at::kInt, {groups}, dev));
+  const int32_t *table = page_table_of(a[5], "page_table", batch, dev, pages, stride);
+  const int32_t *lengths = static_cast<const int32_t *>(plain(a[6], "lengths", at::kInt, {batch}, dev));
+  const tq_scores s = scores_of(a[7], nullptr, a[8], a[9], hq, c.c.head_dim, dev);
+  const bool return_lse = to_bool(a[10]);
+  const size_t bytes = L.prefix_bytes(&c.c, batch, hq, groups, prefix_pages, pages);
+  const at::Tensor out = fresh({batch, hq, c.c.head_dim}, qt.scalar_type(), dev);
+  at::Tensor lse, scratch;
+  if (return_lse) lse = fresh({batch, hq}, at::kFloat, dev);
+  if (bytes > 0) scratch = fresh({(int64_t)((bytes + 3) / 4)}, at::kFloat, dev);
+  if (batch > 0)
+    check(L.prefix(&c.c, &q, dtype_of(qt.scalar_type()), batch, hq, groups, members, prefix_table, prefix_stride, prefix_pages,
+                   prefix_lengths, table, stride, pages, lengths, &s, out.data_ptr(),
+                   return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, bytes > 0 ? scratch.data_ptr() : nullptr,
+                   to_stream(a[12])),
+          "tq_shared_prefix_attention");
+  return return_lse ? wrap2(out, lse) : wrap(out);
 }
 
 // prompt(cache, q, starts, page_table, lengths, scale or None, window, prefix or None, first or None, softcap,
@@ -450,9 +475,11 @@ PyObject *bind(PyObject *const *a, Py_ssize_t) {
   L.norm_rope_append = reinterpret_cast<decltype(L.norm_rope_append)>(to_stream(a[3]));
   L.read = reinterpret_cast<decltype(L.read)>(to_stream(a[4]));
   L.scratch_bytes = reinterpret_cast<decltype(L.scratch_bytes)>(to_stream(a[5]));
-  L.attend = reinterpret_cast<decltype(L.attend)>(to_stream(a[6]));
-  L.prompt_bytes = reinterpret_cast<decltype(L.prompt_bytes)>(to_stream(a[7]));
-  L.prompt = reinterpret_cast<decltype(L.prompt)>(to_stream(a[8]));
+  L.prompt_bytes = reinterpret_cast<decltype(L.prompt_bytes)>(to_stream(a[6]));
+  L.prompt = reinterpret_cast<decltype(L.prompt)>(to_stream(a[7]));
+  L.attend_scored = reinterpret_cast<decltype(L.attend_scored)>(to_stream(a[8]));
+  L.prefix_bytes = reinterpret_cast<decltype(L.prefix_bytes)>(to_stream(a[9]));
+  L.prefix = reinterpret_cast<decltype(L.prefix)>(to_stream(a[10]));
   Py_RETURN_NONE;
 }
 
@@ -480,8 +507,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define TQ_METHOD(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TQ_METHOD(bind, 10), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
-                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 9), TQ_METHOD(prompt, 14),
+PyMethodDef methods[] = {TQ_METHOD(bind, 12), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
+                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 11), TQ_METHOD(prompt, 14), TQ_METHOD(prefix, 13),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

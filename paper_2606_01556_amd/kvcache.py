@@ -25,7 +25,8 @@ import os
 from . import TQError, _HERE, _other_stream, _stream, lib
 
 __all__ = ["KVCache", "empty_kv_cache", "rope_table", "kv_append", "kv_read", "qk_norm_rope",
-           "qk_norm_rope_append", "paged_attention", "prompt_attention"]
+           "qk_norm_rope_append", "paged_attention", "prompt_attention",
+           "shared_prefix_attention"]
 
 
 class _CacheDesc(ctypes.Structure):     # tq_kv_cache
@@ -62,6 +63,10 @@ def declare(L):
     L.tq_paged_attention_scratch_bytes.restype = ctypes.c_size_t
     L.tq_paged_attention.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, ctypes.c_float, I, P, P, P, P]
     S = ctypes.POINTER(_Scores)
+    L.tq_paged_attention_scored.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, S, P, P, P, P]
+    L.tq_shared_prefix_attention_scratch_bytes.argtypes = [C, I, I, I, I, I]
+    L.tq_shared_prefix_attention_scratch_bytes.restype = ctypes.c_size_t
+    L.tq_shared_prefix_attention.argtypes = [C, H, I, I, I, I, P, P, ctypes.c_int64, I, P, P, ctypes.c_int64, I, P, S, P, P, P, P]
     L.tq_prompt_attention_scratch_bytes.argtypes = [C, I, I, I, I, I]
     L.tq_prompt_attention_scratch_bytes.restype = ctypes.c_size_t
     L.tq_prompt_attention.argtypes = [C, H, I, I, I, I, P, P, ctypes.c_int64, I, P, P, P, S, P, P, P, P]
@@ -85,8 +90,8 @@ def _load():
     L = lib()
     native.bind(TQError, torch.OutOfMemoryError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.tq_qk_norm_rope, L.tq_kv_append, L.tq_qk_norm_rope_append, L.tq_kv_read,
-        L.tq_paged_attention_scratch_bytes, L.tq_paged_attention, L.tq_prompt_attention_scratch_bytes,
-        L.tq_prompt_attention)))
+        L.tq_paged_attention_scratch_bytes, L.tq_prompt_attention_scratch_bytes, L.tq_prompt_attention,
+        L.tq_paged_attention_scored, L.tq_shared_prefix_attention_scratch_bytes, L.tq_shared_prefix_attention)))
     _torch, _get_device, _get_raw = torch, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _native = native
     return native
@@ -243,18 +248,19 @@ def qk_norm_rope_append(cache: KVCache, q, k, v, positions, table, slots, q_weig
 
 
 def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None = None, window: int = 0,
-                    return_lse: bool = False, stream=None):
-    """Attention of one new token of every stream over the cache (tq_paged_attention):
-    q [batch, q_heads, head_dim], page_table [batch, max_pages] int32 (rows may be
+                    return_lse: bool = False, stream=None, *, softcap: float = 0.0, slopes=None):
+    """Attention of one new token of every stream over the cache (tq_paged_attention): q [batch, q_heads, head_dim], page_table [batch, max_pages] int32 (rows may be
     strided), lengths [batch] int32 the tokens of each stream, its newest one among
-    them.  window > 0: only the last so many.  scale: head_dim^-1/2 by default.
+    them.  window > 0: only the last so many.  scale: head_dim^-1/2 by default.  softcap >
+    0: scores s become softcap * tanh(s / softcap); slopes [q_heads] float32: less slopes[h]
+    times the distance (tq_paged_attention_scored).
     Returns out [batch, q_heads, head_dim] of q's type, zeros for a stream of length
     0; with return_lse (out, lse [batch, q_heads] float32)."""
     c = _handle(cache)
     if stream is not None:
-        return _elsewhere(stream, (q, page_table, lengths, *cache._t), lambda dev, st: _native.attend(
-            c, q, page_table, lengths, scale, window, return_lse, dev, st))
-    return _native.attend(c, q, page_table, lengths, scale, window, return_lse, *_here())
+        return _elsewhere(stream, (q, page_table, lengths, slopes, *cache._t), lambda dev, st: _native.attend(
+            c, q, page_table, lengths, scale, window, return_lse, softcap, slopes, dev, st))
+    return _native.attend(c, q, page_table, lengths, scale, window, return_lse, softcap, slopes, *_here())
 
 
 def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: float | None = None, window: int = 0,
@@ -281,3 +287,26 @@ def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: floa
                                                          softcap, slopes, return_lse, dev, st))
     return _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first, softcap, slopes, return_lse,
                           *_here())
+
+
+def shared_prefix_attention(cache: KVCache, q, members, prefix_table, prefix_lengths, page_table, lengths,
+                            scale: float | None = None, softcap: float = 0.0, slopes=None, return_lse: bool = False,
+                            stream=None):
+    """Attention of one new token of every stream, q [batch, q_heads, head_dim], over a
+    prefix that its group shares, read once for the group, and over the stream's own
+    tokens behind it (tq_shared_prefix_attention).  Group g's streams are rows members[g]
+    to members[g + 1] (members [groups + 1] int32; a stream of no group has no prefix), its
+    prefix the first prefix_lengths[g] tokens of the pages prefix_table[g] (prefix_table
+    [groups, prefix_pages] int32).  page_table and lengths: the streams' own tokens, the
+    newest among them, as in ``paged_attention``; scale, softcap and slopes as there, with
+    distances across the prefix.
+
+    Returns out [batch, q_heads, head_dim] of q's type, zeros for a stream without prefix
+    and tokens; with return_lse (out, lse [batch, q_heads] float32)."""
+    c = _handle(cache)
+    if stream is not None:
+        return _elsewhere(stream, (q, members, prefix_table, prefix_lengths, page_table, lengths, slopes, *cache._t),
+                          lambda dev, st: _native.prefix(c, q, members, prefix_table, prefix_lengths, page_table, lengths,
+                                                         scale, softcap, slopes, return_lse, dev, st))
+    return _native.prefix(c, q, members, prefix_table, prefix_lengths, page_table, lengths, scale, softcap, slopes,
+                          return_lse, *_here())
