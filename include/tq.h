@@ -508,6 +508,33 @@ tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q
                                      int64_t table_stride, int max_pages, const int32_t *lengths,
                                      const tq_scores *scores, void *out, float *lse, void *scratch, void *stream);
 
+/* Between two blocks of a decoder, rows of n values of 16 bits; strides in values,
+ * multiples of 8, rows contiguous and starting on 16 bytes. */
+typedef struct {
+    const void *x;             /* [tokens, n] a block's result                                   */
+    int64_t x_stride;
+    const void *residual;      /* [tokens, n] the residual stream, or NULL (zeros)               */
+    int64_t residual_stride;
+    const void *gate;          /* [tokens, n], with gate_stride 0 [n] for all tokens, or NULL     */
+    int64_t gate_stride;
+    const void *post_weight;   /* [n] of the norm after the block, or NULL (no norm)             */
+    const void *weight;        /* [n] of the norm before the next block                          */
+    float scale, eps;          /* of the block's share; of both norms                            */
+} tq_residual_norm;
+
+/* One launch:
+ *   z = x / sqrt(mean(x^2) + eps) * post_weight * gate     (x where there is no post_weight)
+ *   sum = residual + scale * z
+ *   normed = sum / sqrt(mean(sum^2) + eps) * weight
+ * in fp32, each result rounded once (normed is made of the sum before its rounding).
+ *   sum, normed  [tokens, n] contiguous, of type dtype; either may be NULL (not both), and be
+ *                x or residual where those are contiguous.  normed needs weight
+ * n a multiple of 8 up to 32768; tokens == 0 is a no-op.
+ * Errors: TQ_ERR_NULL, TQ_ERR_SHAPE (sizes, eps negative or not finite, scale not finite),
+ * TQ_ERR_DTYPE, TQ_ERR_ALIGN, TQ_ERR_HIP. */
+tq_status tq_add_rms_norm(const tq_residual_norm *p, int tokens, int n, tq_dtype dtype, void *sum, void *normed,
+                          void *stream);
+
 /* Static description of a status code; never NULL. */
 const char *tq_status_string(tq_status s);
 

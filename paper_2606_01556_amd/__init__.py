@@ -49,7 +49,8 @@ EXPORTS = ("tq_weight_desc_init", "tq_pack_weights", "tq_quant_act", "tq_dual_ge
            "tq_export_weights_canonical", "tq_act_codes_canonical", "tq_layer",
            "tq_layer_scratch_bytes", "tq_qk_norm_rope", "tq_kv_append", "tq_qk_norm_rope_append", "tq_kv_read",
            "tq_paged_attention_scratch_bytes", "tq_paged_attention", "tq_prompt_attention_scratch_bytes", "tq_prompt_attention",
-           "tq_paged_attention_scored", "tq_shared_prefix_attention_scratch_bytes", "tq_shared_prefix_attention")
+           "tq_paged_attention_scored", "tq_shared_prefix_attention_scratch_bytes", "tq_shared_prefix_attention",
+           "tq_add_rms_norm")
 
 _lib = None
 
@@ -539,5 +540,5 @@ def act_codes_rows(x_codes, m: int) -> np.ndarray:
 
 
 from . import kvcache                                                          # noqa: E402
-from .kvcache import (KVCache, empty_kv_cache, kv_append, kv_read, paged_attention,   # noqa: E402,F401
+from .kvcache import (KVCache, add_rms_norm, empty_kv_cache, kv_append, kv_read, paged_attention,   # noqa: E402,F401
                       prompt_attention, qk_norm_rope, qk_norm_rope_append, rope_table, shared_prefix_attention)

@@ -102,6 +102,18 @@ struct PromptArgs {
 // floats of the references and sums in front of the products (which start on 16 bytes)
 __host__ __device__ inline int64_t parts_head(int splits, int64_t heads) { return (2 * splits * heads + 3) & ~(int64_t)3; }
 
+// Rows between two blocks; strides in values.
+constexpr int kNormMost = 32768;   // values of a row
+struct NormArgs {
+  const uint16_t *x, *residual, *gate;   // [tokens][n]; residual and gate may be null
+  int64_t x_stride, r_stride, g_stride;  // g_stride 0: one row
+  const uint16_t *post, *weight;         // [n] or null
+  float scale, eps;
+  int tokens, n;
+  uint16_t *sum, *normed;                // [tokens][n]; either may be null
+};
+hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t s);
+
 hipError_t launch_tokens(const TokenArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_kv_read(const ReadArgs &a, bool bf16, hipStream_t s);
 // How an attention call is cut, by what the host knows of it: direct, one

@@ -359,4 +359,41 @@ tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q
   return hip_status(tq::launch_prefix(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
+tq_status tq_add_rms_norm(const tq_residual_norm *p, int tokens, int n, tq_dtype dtype, void *sum, void *normed, void *stream) {
+  if (p == nullptr || p->x == nullptr || (sum == nullptr && normed == nullptr) || (normed != nullptr && p->weight == nullptr))
+    return TQ_ERR_NULL;
+  if (tokens < 0 || n < 8 || n > tq::kNormMost || n % 8 != 0) return TQ_ERR_SHAPE;
+  if (!(p->eps >= 0.0f) || std::isinf(p->eps) || !std::isfinite(p->scale)) return TQ_ERR_SHAPE;
+  if (!dtype_ok(dtype)) return TQ_ERR_DTYPE;
+  if (((p->x_stride | p->residual_stride | p->gate_stride) & 7) != 0) return TQ_ERR_ALIGN;
+  for (const void *at : {p->x, p->residual, p->gate, p->post_weight, p->weight, (const void *)sum, (const void *)normed})
+    if (!aligned16(at)) return TQ_ERR_ALIGN;
+  if (tokens == 0) return TQ_OK;
+  tq::NormArgs a = {};
+  a.x = static_cast<const uint16_t *>(p->x); a.x_stride = p->x_stride;
+  a.residual = static_cast<const uint16_t *>(p->residual); a.r_stride = p->residual_stride;
+  a.gate = static_cast<const uint16_t *>(p->gate); a.g_stride = p->gate_stride;
+  a.post = static_cast<const uint16_t *>(p->post_weight);
+  a.weight = static_cast<const uint16_t *>(p->weight);
+  a.scale = p->scale; a.eps = p->eps;
+  a.tokens = tokens; a.n = n;
+  a.sum = static_cast<uint16_t *>(sum);
+  a.normed = static_cast<uint16_t *>(normed);
+  // (a launch numbers its lanes in 32 bits: rows of up to 1024 lanes go in runs)
+  const int most = 1 << 21;
+  for (int done = 0; done < tokens; done += most) {
+    tq::NormArgs b = a;
+    b.tokens = tokens - done < most ? tokens - done : most;
+    b.x += done * a.x_stride;
+    if (a.residual != nullptr) b.residual += done * a.r_stride;
+    if (a.gate != nullptr) b.gate += done * a.g_stride;
+    if (a.sum != nullptr) b.sum += (int64_t)done * n;
+    if (a.normed != nullptr) b.normed += (int64_t)done * n;
+    const tq_status st = hip_status(tq::launch_norm(b, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
+    if (st != TQ_OK) return st;
+    if (tokens - done <= most) break;
+  }
+  return TQ_OK;
+}
+
 }  // extern "C"

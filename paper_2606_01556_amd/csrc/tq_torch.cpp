@@ -43,6 +43,7 @@ struct Entries {
   decltype(&tq_paged_attention_scored) attend_scored;
   decltype(&tq_shared_prefix_attention_scratch_bytes) prefix_bytes;
   decltype(&tq_shared_prefix_attention) prefix;
+  decltype(&tq_add_rms_norm) add_norm;
 } L;
 PyObject *tq_error;         // TQError(code, where)
 PyObject *out_of_memory;    // torch's
@@ -463,6 +464,55 @@ PyObject *prompt(PyObject *const *a, Py_ssize_t) {
   return return_lse ? wrap2(out, lse) : wrap(out);
 }
 
+// rows [tokens, n] of one type, the last axis contiguous: address and stride
+const void *wide_rows(PyObject *o, const char *name, at::ScalarType type, int64_t tokens, int64_t n, int64_t dev, int64_t &stride) {
+  const at::Tensor &t = tensor(o, name);
+  on_gpu(t, name, dev);
+  if (t.scalar_type() != type) bad_dtype(t, name, c10::toString(type));
+  if (t.dim() != 2 || t.size(0) != tokens || t.size(1) != n)
+    fail(PyExc_ValueError, "%s: shape %s, expected [%lld, %lld]", name, shape_of(t).c_str(), (long long)tokens, (long long)n);
+  stride = tokens > 1 ? t.stride(0) : 0;
+  if (t.stride(1) != 1 || (stride & 7) != 0 || (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15) != 0)
+    fail(PyExc_ValueError, "%s: rows must be contiguous and start on 16 bytes (strides %lld, %lld); pass %s.contiguous()", name,
+         (long long)t.stride(0), (long long)t.stride(1), name);
+  return t.data_ptr();
+}
+
+// add_norm(x, residual or None, weight or None, post_weight or None, gate or None, scale, eps, return_sum, device, stream):
+// sum, normed or (sum, normed)
+PyObject *add_norm(PyObject *const *a, Py_ssize_t) {
+  const int64_t dev = to_int(a[8]);
+  const at::Tensor &xt = tensor(a[0], "x");
+  on_gpu(xt, "x", dev);
+  const at::ScalarType type = xt.scalar_type();
+  if (!half(type)) bad_dtype(xt, "x", "Half or BFloat16");
+  if (xt.dim() != 2) fail(PyExc_ValueError, "x: shape %s, expected [tokens, n]", shape_of(xt).c_str());
+  const int64_t n = xt.size(1);
+  const int tokens = size32(xt.size(0), "x");
+  if (n < 8 || n > 32768 || n % 8 != 0) fail(PyExc_ValueError, "x: rows of %lld values; a multiple of 8 up to 32768", (long long)n);
+  tq_residual_norm p = {};
+  p.x = wide_rows(a[0], "x", type, tokens, n, dev, p.x_stride);
+  if (a[1] != Py_None) p.residual = wide_rows(a[1], "residual", type, tokens, n, dev, p.residual_stride);
+  p.weight = plain_or_null(a[2], "weight", type, {n}, dev);
+  p.post_weight = plain_or_null(a[3], "post_weight", type, {n}, dev);
+  if (a[4] != Py_None) {
+    if (tensor(a[4], "gate").dim() == 1) p.gate = plain(a[4], "gate", type, {n}, dev);
+    else p.gate = wide_rows(a[4], "gate", type, tokens, n, dev, p.gate_stride);
+  }
+  p.scale = (float)to_double(a[5]);
+  p.eps = (float)to_double(a[6]);
+  const bool return_sum = to_bool(a[7]);
+  if (!return_sum && p.weight == nullptr) fail(PyExc_ValueError, "weight: missing, and the sum is not asked for");
+  at::Tensor sum, normed;
+  if (return_sum) sum = fresh({tokens, n}, type, dev);
+  if (p.weight != nullptr) normed = fresh({tokens, n}, type, dev);
+  if (tokens > 0)
+    check(L.add_norm(&p, tokens, (int)n, dtype_of(type), return_sum ? sum.data_ptr() : nullptr,
+                     p.weight != nullptr ? normed.data_ptr() : nullptr, to_stream(a[9])),
+          "tq_add_rms_norm");
+  return p.weight == nullptr ? wrap(sum) : return_sum ? wrap2(sum, normed) : wrap(normed);
+}
+
 // bind(TQError, torch.OutOfMemoryError, addresses of the entry points, in the order of Entries)
 PyObject *bind(PyObject *const *a, Py_ssize_t) {
   Py_INCREF(a[0]);
@@ -480,6 +530,7 @@ PyObject *bind(PyObject *const *a, Py_ssize_t) {
   L.attend_scored = reinterpret_cast<decltype(L.attend_scored)>(to_stream(a[8]));
   L.prefix_bytes = reinterpret_cast<decltype(L.prefix_bytes)>(to_stream(a[9]));
   L.prefix = reinterpret_cast<decltype(L.prefix)>(to_stream(a[10]));
+  L.add_norm = reinterpret_cast<decltype(L.add_norm)>(to_stream(a[11]));
   Py_RETURN_NONE;
 }
 
@@ -507,8 +558,8 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define TQ_METHOD(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, n>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TQ_METHOD(bind, 12), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
-                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 11), TQ_METHOD(prompt, 14), TQ_METHOD(prefix, 13),
+PyMethodDef methods[] = {TQ_METHOD(bind, 13), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
+                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 11), TQ_METHOD(prompt, 14), TQ_METHOD(prefix, 13), TQ_METHOD(add_norm, 10),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

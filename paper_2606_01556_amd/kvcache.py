@@ -26,7 +26,7 @@ from . import TQError, _HERE, _other_stream, _stream, lib
 
 __all__ = ["KVCache", "empty_kv_cache", "rope_table", "kv_append", "kv_read", "qk_norm_rope",
            "qk_norm_rope_append", "paged_attention", "prompt_attention",
-           "shared_prefix_attention"]
+           "shared_prefix_attention", "add_rms_norm"]
 
 
 class _CacheDesc(ctypes.Structure):     # tq_kv_cache
@@ -51,6 +51,13 @@ class _Scores(ctypes.Structure):        # tq_scores
                 ("window", ctypes.c_int32)]
 
 
+class _ResidualNorm(ctypes.Structure):  # tq_residual_norm
+    _fields_ = [("x", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("residual", ctypes.c_void_p),
+                ("residual_stride", ctypes.c_int64), ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64),
+                ("post_weight", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("scale", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
 def declare(L):
     """Argument types of this module's entry points (called as the library loads)."""
     P, I = ctypes.c_void_p, ctypes.c_int
@@ -63,6 +70,7 @@ def declare(L):
     L.tq_paged_attention_scratch_bytes.restype = ctypes.c_size_t
     L.tq_paged_attention.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, ctypes.c_float, I, P, P, P, P]
     S = ctypes.POINTER(_Scores)
+    L.tq_add_rms_norm.argtypes = [ctypes.POINTER(_ResidualNorm), I, I, I, P, P, P]
     L.tq_paged_attention_scored.argtypes = [C, H, I, I, I, P, ctypes.c_int64, I, P, S, P, P, P, P]
     L.tq_shared_prefix_attention_scratch_bytes.argtypes = [C, I, I, I, I, I]
     L.tq_shared_prefix_attention_scratch_bytes.restype = ctypes.c_size_t
@@ -91,7 +99,8 @@ def _load():
     native.bind(TQError, torch.OutOfMemoryError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         L.tq_qk_norm_rope, L.tq_kv_append, L.tq_qk_norm_rope_append, L.tq_kv_read,
         L.tq_paged_attention_scratch_bytes, L.tq_prompt_attention_scratch_bytes, L.tq_prompt_attention,
-        L.tq_paged_attention_scored, L.tq_shared_prefix_attention_scratch_bytes, L.tq_shared_prefix_attention)))
+        L.tq_paged_attention_scored, L.tq_shared_prefix_attention_scratch_bytes, L.tq_shared_prefix_attention,
+        L.tq_add_rms_norm)))
     _torch, _get_device, _get_raw = torch, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _native = native
     return native
@@ -310,3 +319,20 @@ def shared_prefix_attention(cache: KVCache, q, members, prefix_table, prefix_len
                                                          scale, softcap, slopes, return_lse, dev, st))
     return _native.prefix(c, q, members, prefix_table, prefix_lengths, page_table, lengths, scale, softcap, slopes,
                           return_lse, *_here())
+
+
+def add_rms_norm(x, residual=None, weight=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,
+                 return_sum: bool = True, stream=None):
+    """The end of a block and the beginning of the next, in one pass (tq_add_rms_norm): x
+    [tokens, n], normed (RMS, post_weight [n]; None: no norm), times gate ([n], [tokens, n]
+    or None) and scale, added to residual [tokens, n] (None: zeros), and the sum normed
+    again (weight [n]) for what comes next.  fp32 inside, each result rounded once; n a
+    multiple of 8 up to 32768; rows may be strided.
+
+    Returns (sum, normed); sum alone without weight, normed alone without return_sum (which
+    with x and weight only is the plain RMS norm)."""
+    native = _native or _load()
+    if stream is not None:
+        return _elsewhere(stream, (x, residual, weight, post_weight, gate), lambda dev, st: native.add_norm(
+            x, residual, weight, post_weight, gate, scale, eps, return_sum, dev, st))
+    return native.add_norm(x, residual, weight, post_weight, gate, scale, eps, return_sum, *_here())
