@@ -1,11 +1,13 @@
 """A decoder block with quantized layers, from prompts to generated tokens.
 
-The seven projections are the package's W4A4 layers; between them run its head norms
-and rotation, its paged key-value cache (16, 8 or 4 bits) and its attention of the
-newest token.  RMS norms, the prompts' own attention and the MLP's activation are
-torch's.  Weights and inputs are random, of Qwen3-8B's sizes by default.
+The seven projections are the package's W4A4 layers; between them run its norms and
+residual sums, its head norms and rotation, its paged key-value cache (16, 8 or 4 bits)
+and its attentions: of prompts, of the newest token, and of that over a prefix that all
+streams share.  The MLP's activation is torch's.  Weights and inputs are random, of
+Qwen3-8B's sizes by default.
 
     python3 examples/decode_block.py --bits 4 --streams 32 --prompt 1000 --tokens 64 --graph
+    python3 examples/decode_block.py --streams 32 --shared 8192 --prompt 100 --tokens 64 --graph
 
 prints the time of a decode step.  ``Block`` is what a program would keep.
 """
@@ -24,15 +26,23 @@ import paper_2606_01556_amd as tq                                              #
 
 class Pages:
     """Which pages of a cache each stream holds: a program's block manager, at its
-    simplest."""
+    simplest.  `shared` tokens (whole pages) that all streams begin with are held once."""
 
-    def __init__(self, streams: int, tokens: int, page_size: int, seed: int = 0):
-        self.page_size, self.each = page_size, -(-tokens // page_size)
-        order = torch.randperm(streams * self.each, generator=torch.Generator().manual_seed(seed))
-        self.table = order.view(streams, self.each).to(torch.int32).cuda()
+    def __init__(self, streams: int, tokens: int, page_size: int, seed: int = 0, shared: int = 0):
+        assert shared % page_size == 0, "a shared prefix ends with a page"
+        self.page_size, self.each, self.shared = page_size, -(-tokens // page_size), shared
+        front = shared // page_size
+        order = torch.randperm(front + streams * self.each, generator=torch.Generator().manual_seed(seed)).to(torch.int32).cuda()
+        self.count = order.numel()
+        self.prefix, self.table = order[None, :front], order[front:].view(streams, self.each)
+        # what a stream's tokens attend to as one sequence: the shared pages, then its own
+        self.whole = torch.cat((self.prefix.expand(streams, -1), self.table), 1).contiguous()
+        self.members = torch.tensor([0, streams], dtype=torch.int32, device="cuda")
+        self.prefix_lengths = torch.tensor([shared], dtype=torch.int32, device="cuda")
 
     def slots(self, stream, position):
-        """Slot numbers of (stream, position) pairs, both int64."""
+        """Slot numbers of (stream, position) pairs, both int64, positions counted from the
+        end of what is shared."""
         page = self.table[stream, position // self.page_size].long()
         return page * self.page_size + position % self.page_size
 
@@ -63,67 +73,76 @@ class Block:
         if head_norms:
             self.q_norm = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).half()
             self.k_norm = (1 + 0.1 * torch.randn(d, generator=gen, device="cuda")).half()
+        self.attention_norm, self.mlp_norm = (torch.ones(hidden, device="cuda").half() for _ in range(2))
         self.rope = tq.rope_table(positions, d, base=1e6)
         self.cache = tq.empty_kv_cache(pages, page_size, kv_heads, d, bits)
 
     def heads_of(self, x):
         """q, k and v [tokens, heads, head_dim]: views of the fused projection."""
-        y = self.qkv(rms_norm(x)).view(x.shape[0], -1, self.d)
+        y = self.qkv(tq.add_rms_norm(x, weight=self.attention_norm, return_sum=False)).view(x.shape[0], -1, self.d)
         return y.split((self.heads, self.kv_heads, self.kv_heads), 1)
 
     def rest(self, x, attended):
-        x = x + self.o(attended.reshape(x.shape[0], -1))
-        h = rms_norm(x)
-        return x + self.down((torch.nn.functional.silu(self.gate(h).float()) * self.up(h)).half())
+        x, h = tq.add_rms_norm(self.o(attended.reshape(x.shape[0], -1)), x, self.mlp_norm)
+        return tq.add_rms_norm(self.down((torch.nn.functional.silu(self.gate(h).float()) * self.up(h)).half()), x)
 
-    def prompt(self, x, positions, slots, streams):
-        """x [streams * length, hidden]: prompts of one length, written to the cache and
-        attended to among themselves (by torch: k as it was before the cache's quantizer)."""
-        q, k, v = self.heads_of(x)
-        q, k = tq.qk_norm_rope_append(self.cache, q, k, v, positions, self.rope, slots, self.q_norm, self.k_norm,
-                                      return_k=True)
-        group = self.heads // self.kv_heads
-        q, k, v = (t.reshape(streams, -1, t.shape[1], self.d).transpose(1, 2).float() for t in (q, k, v))
-        k, v = (t.repeat_interleave(group, 1) for t in (k, v))
-        y = torch.nn.functional.scaled_dot_product_attention(q, k, v, is_causal=True)
-        return self.rest(x, y.transpose(1, 2).half())
-
-    def decode(self, x, positions, slots, page_table, lengths):
-        """x [streams, hidden]: one new token of every stream, at `positions` and in
-        `slots`; lengths count it."""
+    def prompt(self, x, positions, slots, starts, page_table, lengths):
+        """x [tokens, hidden]: new tokens of streams, one stream after the other from rows
+        `starts` on, the last of each stream's `lengths`: written to the cache, and
+        attended to as the cache holds them."""
         q, k, v = self.heads_of(x)
         q = tq.qk_norm_rope_append(self.cache, q, k, v, positions, self.rope, slots, self.q_norm, self.k_norm)
-        return self.rest(x, tq.paged_attention(self.cache, q, page_table, lengths))
+        return self.rest(x, tq.prompt_attention(self.cache, q, starts, page_table, lengths))
+
+    def decode(self, x, positions, slots, page_table, lengths, pages=None):
+        """x [streams, hidden]: one new token of every stream, at `positions` and in
+        `slots`; lengths count it.  pages: whose prefix the streams share."""
+        q, k, v = self.heads_of(x)
+        q = tq.qk_norm_rope_append(self.cache, q, k, v, positions, self.rope, slots, self.q_norm, self.k_norm)
+        if pages is None:
+            return self.rest(x, tq.paged_attention(self.cache, q, page_table, lengths))
+        return self.rest(x, tq.shared_prefix_attention(self.cache, q, pages.members, pages.prefix, pages.prefix_lengths,
+                                                       page_table, lengths))
 
 
-def captured(block, x, positions, slots, page_table, lengths):
+def captured(block, *tensors):
     """A graph of one decode step over these tensors, and the tensor of its result."""
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):                 # everything the step loads or sets up, first
-        block.decode(x, positions, slots, page_table, lengths)
+        block.decode(*tensors)
     torch.cuda.current_stream().wait_stream(side)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        y = block.decode(x, positions, slots, page_table, lengths)
+        y = block.decode(*tensors)
     return graph, y
 
 
-def generate(block, pages, x, tokens, graph=False):
+def generate(block, pages, x, tokens, graph=False, shared=None):
     """The block's outputs for prompts x [streams, length, hidden] and for `tokens` new
     tokens of each stream (the block's last output taken as its next input, as there
-    is no vocabulary here): [streams, length + tokens, hidden], and seconds a token."""
+    is no vocabulary here): [streams, length + tokens, hidden], and seconds a token.
+    shared [pages.shared, hidden]: what all prompts begin with, computed once."""
     streams, length, hidden = x.shape
+    front = pages.shared
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    if front:
+        position = torch.arange(front, device="cuda")
+        slots = pages.prefix[0, position // pages.page_size].long() * pages.page_size + position % pages.page_size
+        block.prompt(shared, position.to(torch.int32), slots, ints(0, front), pages.prefix, ints(front))
     stream = torch.arange(streams, device="cuda")
     position = torch.arange(length, device="cuda")
     slots = pages.slots(stream.repeat_interleave(length), position.repeat(streams))
-    y = block.prompt(x.reshape(-1, hidden), position.repeat(streams).to(torch.int32), slots, streams)
+    starts = torch.arange(0, streams * length + 1, length, dtype=torch.int32, device="cuda")
+    y = block.prompt(x.reshape(-1, hidden), (front + position).repeat(streams).to(torch.int32), slots, starts, pages.whole,
+                     torch.full((streams,), front + length, dtype=torch.int32, device="cuda"))
     out = [y.view(streams, length, hidden)]
     # what a step reads: kept tensors, which a graph needs
     new = rms_norm(out[0][:, -1]).contiguous()
-    positions = torch.full((streams,), length, dtype=torch.int32, device="cuda")
-    lengths, slots = positions + 1, pages.slots(stream, positions.long())
-    step = captured(block, new, positions, slots, pages.table, lengths) if graph else None
+    lengths = torch.full((streams,), length + 1, dtype=torch.int32, device="cuda")
+    positions, slots = lengths + (front - 1), pages.slots(stream, (lengths - 1).long())
+    args = (new, positions, slots, pages.table, lengths, pages if front else None)
+    step = captured(block, *args) if graph else None
     torch.cuda.synchronize()
     begin = time.perf_counter()
     for t in range(tokens):
@@ -131,13 +150,13 @@ def generate(block, pages, x, tokens, graph=False):
             step[0].replay()
             y = step[1].clone()
         else:
-            y = block.decode(new, positions, slots, pages.table, lengths)
+            y = block.decode(*args)
         out.append(y[:, None])
         if t + 1 < tokens:
             new.copy_(rms_norm(y))
             positions += 1
             lengths += 1
-            slots.copy_(pages.slots(stream, positions.long()))
+            slots.copy_(pages.slots(stream, (lengths - 1).long()))
     torch.cuda.synchronize()
     return torch.cat(out, 1), (time.perf_counter() - begin) / max(tokens, 1)
 
@@ -149,15 +168,17 @@ def main():
     ap.add_argument("--prompt", type=int, default=512)
     ap.add_argument("--tokens", type=int, default=32)
     ap.add_argument("--page-size", type=int, default=16)
+    ap.add_argument("--shared", type=int, default=0, help="tokens that all prompts begin with, held once")
     ap.add_argument("--graph", action="store_true", help="replay a captured step")
     a = ap.parse_args()
-    pages = Pages(a.streams, a.prompt + a.tokens, a.page_size)
-    block = Block(bits=a.bits, pages=pages.table.numel(), page_size=a.page_size, positions=a.prompt + a.tokens)
-    x = torch.randn(a.streams, a.prompt, 4096, generator=torch.Generator(device="cuda").manual_seed(1),
-                    device="cuda").half()
-    generate(block, pages, x[:, :8], 2, a.graph)
-    y, seconds = generate(block, pages, x, a.tokens, a.graph)
-    print(f"{a.streams} streams of {a.prompt} + {a.tokens} tokens, {a.bits}-bit cache: "
+    pages = Pages(a.streams, a.prompt + a.tokens, a.page_size, shared=a.shared)
+    block = Block(bits=a.bits, pages=pages.count, page_size=a.page_size, positions=a.shared + a.prompt + a.tokens)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(a.streams, a.prompt, 4096, generator=gen, device="cuda").half()
+    shared = torch.randn(a.shared, 4096, generator=gen, device="cuda").half()
+    generate(block, pages, x[:, :8], 2, a.graph, shared)
+    y, seconds = generate(block, pages, x, a.tokens, a.graph, shared)
+    print(f"{a.streams} streams of {a.shared} shared + {a.prompt} + {a.tokens} tokens, {a.bits}-bit cache: "
           f"{seconds * 1e6:.0f} us per decode step of one block; output rms {y.float().square().mean().sqrt():.3f}")
 
 

@@ -91,6 +91,7 @@ struct PromptArgs {
   const float *slopes;       // [hq] or null
   int window;                // 0: none
   bool shared;
+  bool fine;                 // weights in two terms
   uint16_t *out;             // [tokens][hq][d]
   float *lse;                // [tokens][hq] or null
   // parts where splits > 1 or shared: [splits][tokens][hq] references and sums, then as many products [d]

@@ -86,11 +86,21 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return BF16 ? ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u : ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
 }
 
+// the two values of a word
+template <bool BF16>
+__device__ __forceinline__ float lower_half(uint32_t w) {
+  return BF16 ? __builtin_bit_cast(float, w << 16) : half_bits_to_float((uint16_t)w);
+}
+template <bool BF16>
+__device__ __forceinline__ float upper_half(uint32_t w) {
+  return BF16 ? __builtin_bit_cast(float, w & 0xffff0000u) : half_bits_to_float((uint16_t)(w >> 16));
+}
+
 struct Interval {
   int lo, hi;    // empty: INT32_MAX and 0
 };
 
-template <int D, int BITS, bool BF16, bool EXT>
+template <int D, int BITS, bool BF16, bool EXT, bool FINE>
 __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_kernel(const PromptArgs a) {
   constexpr int KT = kTileKeys, W = kPromptWaves, T = kPromptThreads;
   constexpr int RB = D * BITS / 8;              // bytes of a cache row
@@ -233,25 +243,28 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
 #pragma unroll
     for (int i = 0; i < NL; i++) page[i] = pages[held(k + (i * W + w) * LR) >> lps];
   };
-  auto base_of = [&](int i) -> int64_t { return ((int64_t)min(max(page[i], 0), a.c.pages - 1) * hkv + kvh) << lps; };
+  // byte offset of a load's page, from this kv head's rows of page 0
+  const uint32_t page_rows = (uint32_t)hkv << lps;                // <= 2^25 (host)
+  const uint8_t *const kbase = a.c.k + ((int64_t)kvh << lps) * RB, *const vbase = a.c.v + ((int64_t)kvh << lps) * RB;
+  auto base_of = [&](int i) -> int64_t { return (int64_t)((uint64_t)(uint32_t)min(max(page[i], 0), a.c.pages - 1) * page_rows * RB); };
   u32x4 kraw[BITS < 16 ? NL : 1], vraw[BITS < 16 ? NL : 1];       // codes on their way
   uint16_t sraw = 0;
   auto load = [&](int k, uint32_t stage) {
 #pragma unroll
     for (int i = 0; i < NL; i++) {
-      const int64_t base = base_of(i) * RB;
+      const int64_t base = base_of(i);
       const int r = (i * W + w) * LR + lrow;
       const uint32_t off = (uint32_t)(held(k + r) & ((1 << lps) - 1)) * RB;
       if constexpr (BITS == 16) {
         const uint32_t to = stage + (i * W + w) * 1024;
-        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? r & 15 : r & 7)), a.c.k + base, lds0 + to);
-        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3))), a.c.v + base, lds0 + to + VOFF);
+        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? r & 15 : r & 7)), kbase + base, lds0 + to);
+        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3))), vbase + base, lds0 + to + VOFF);
       } else if constexpr (PIECE == 16) {
-        kraw[i] = *reinterpret_cast<const u32x4 *>(a.c.k + base + off + 16 * lpiece);
-        vraw[i] = *reinterpret_cast<const u32x4 *>(a.c.v + base + off + 16 * lpiece);
+        kraw[i] = *reinterpret_cast<const u32x4 *>(kbase + base + off + 16 * lpiece);
+        vraw[i] = *reinterpret_cast<const u32x4 *>(vbase + base + off + 16 * lpiece);
       } else {
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(a.c.k + base + off + 8 * lpiece);
-        const u32x2 y = *reinterpret_cast<const u32x2 *>(a.c.v + base + off + 8 * lpiece);
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(kbase + base + off + 8 * lpiece);
+        const u32x2 y = *reinterpret_cast<const u32x2 *>(vbase + base + off + 8 * lpiece);
         kraw[i] = u32x4{x.x, x.y, 0, 0};
         vraw[i] = u32x4{y.x, y.y, 0, 0};
       }
@@ -359,9 +372,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   const uint32_t count = (uint32_t)max(seen.hi - max(seen.lo, 0), 0) & (seen.lo < seen.hi ? 0xffffffffu : 0u);
   auto masked = [&](int k, int i, int v) -> bool { return (uint32_t)(k + key_of(i, v) - seen.lo) >= count; };
   // the weights of the tile, rounded, in pt; edge: some row does not see all of its keys
-  auto softmax = [&](int k, uint32_t stage, bool edge) {
-    if (edge) {
-      asm volatile("");          // (a branch)
+  auto softmax = [&](int k, uint32_t stage, auto edge) {
+    if constexpr (decltype(edge)::value) {
 #pragma unroll
       for (int i = 0; i < NK; i++)
 #pragma unroll
@@ -416,43 +428,63 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
         }
       }
     l += sum;
-#pragma unroll
-    for (int i = 0; i < NK; i++)
-#pragma unroll
-      for (int t = 0; t < 2; t++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) pt[i][t][j] = pack2<VBF>(sc[i][8 * t + 2 * j], sc[i][8 * t + 2 * j + 1]);
   };
   auto values_of = [&](uint32_t at_lds, int i, int t, int c) -> u32x4 {
     const uint8_t *p = smem + at_lds + (32 * i + 16 * t) * LB + vrow + 16 * ((4 * c + vc) ^ vx);
     const u32x2 x = read_columns(p), y = read_columns(p + 8 * LB);
     return u32x4{x.x, x.y, y.x, y.y};
   };
+  // O^T += V^T P^T: the weights rounded, and (fine) what that leaves of them
   auto products = [&](uint32_t at_lds) {
 #pragma unroll
-    for (int c = 0; c < DT; c++)
+    for (int term = 0; term < (FINE ? 2 : 1); term++) {
 #pragma unroll
       for (int i = 0; i < NK; i++)
 #pragma unroll
-        for (int t = 0; t < 2; t++) o[c] = mfma32<VBF>(values_of(at_lds, i, t, c), pt[i][t], o[c]);
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            float x = sc[i][8 * t + 2 * j], y = sc[i][8 * t + 2 * j + 1];
+            if (term > 0) {
+              x -= lower_half<VBF>(pt[i][t][j]);
+              y -= upper_half<VBF>(pt[i][t][j]);
+            }
+            pt[i][t][j] = pack2<VBF>(x, y);
+          }
+#pragma unroll
+      for (int c = 0; c < DT; c++)
+#pragma unroll
+        for (int i = 0; i < NK; i++)
+#pragma unroll
+          for (int t = 0; t < 2; t++) o[c] = mfma32<VBF>(values_of(at_lds, i, t, c), pt[i][t], o[c]);
+    }
   };
 
-  // ---- the tiles
-  if (k0 < k1) {
-    load_pages(k0);
-    load(k0, 0);
-    widen(0);
-    load_pages(min(k0 + KT, k1 - 1));
+  // ---- the tiles: first those that all rows see whole, [p0, p1), then the others
+  int p0 = k0, p1 = k0;
+  if (all_lo_max < all_hi_min) {
+    p0 = min(k0 + max(all_lo_max - k0 + KT - 1, 0) / KT * KT, k1);
+    p1 = max(min(k0 + max(all_hi_min - k0, 0) / KT * KT, k1), p0);
   }
+  const int skip = p1 - p0;
+  // the t-th of all tiles in that order, t counted in keys (past the last one: any)
+  auto tile_at = [&](int t) -> int { return t < skip ? p0 + t : t - skip < p0 - k0 ? k0 + t - skip : k0 + t; };
+  const int end = k1 - k0;
   uint32_t stage = 0;
-  for (int k = k0; k < k1; k += KT) {
+  if (end > 0) {
+    load_pages(tile_at(0));
+    load(tile_at(0), 0);
+    widen(0);
+    load_pages(tile_at(KT));
+  }
+  int t = 0;
+  // a tile's data is there, and the next one's on its way
+  auto next = [&]() {
     wait_all();
-    const bool more = k + KT < k1;
-    if (more) {
-      load(k + KT, STAGE - stage);
-      load_pages(min(k + 2 * KT, k1 - 1));
+    if (t + KT < end) {
+      load(tile_at(t + KT), STAGE - stage);
+      load_pages(tile_at(t + 2 * KT));
     }
-    const bool here = live && k < hi_max && k + KT > lo_min, edge = k < lo_max || k + KT > hi_min;
     if constexpr (BITS < 16) {
       // rows whose value scale is NaN read as NaN
       const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + stage + SOFF + 12 * KT);
@@ -462,31 +494,40 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
         wait_lds();
       }
     }
-    bool odd = false;            // a value is not finite, and not all rows see all keys
-    if (k < all_lo_max || k + KT > all_hi_min) {
-      uint32_t bad = 0;
-#pragma unroll
-      for (int i = 0; i < KT * LB / (16 * T); i++) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
-#pragma unroll
-        for (int j = 0; j < 4; j++) bad |= not_finite<VBF>(x[j]);
-      }
-      if (__any(bad != 0) && lane == 0) *flag = k / KT + 1;
-      wait_lds();
-      odd = uniform(*flag) == k / KT + 1;
+  };
+  auto done = [&]() {
+    if (t + KT < end) widen(STAGE - stage);
+    stage = STAGE - stage;
+  };
+  for (; t < skip; t += KT) {
+    next();
+    if (live) {
+      scores(tile_at(t), stage);
+      softmax(tile_at(t), stage, std::false_type());
+      products(stage + VOFF);
     }
-    if (!odd) {
-      if (here) {
-        scores(k, stage);
-        softmax(k, stage, edge);
-        products(stage + VOFF);
-      }
-    } else {
-      if (here) {
-        scores(k, stage);
-        softmax(k, stage, edge);
-      }
-      wait_lds();                // the keys have been read: their place takes ones where a value is not finite
+    done();
+  }
+  for (; t < end; t += KT) {
+    next();
+    const int k = tile_at(t);
+    const bool here = live && k < hi_max && k + KT > lo_min;
+    // is a value not finite?
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < KT * LB / (16 * T); i++) {
+      const u32x4 x = *reinterpret_cast<const u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
+#pragma unroll
+      for (int j = 0; j < 4; j++) bad |= not_finite<VBF>(x[j]);
+    }
+    if (__any(bad != 0) && lane == 0) *flag = t + 1;
+    if (here) {
+      scores(k, stage);
+      softmax(k, stage, std::true_type());
+    }
+    wait_lds();
+    if (uniform(*flag) == t + 1) {
+      // the keys have been read: their place takes ones where a value is not finite
 #pragma unroll
       for (int i = 0; i < KT * LB / (16 * T); i++) {
         u32x4 *const v = reinterpret_cast<u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
@@ -502,28 +543,28 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
       }
       wait_lds();
       if (here) {
-        products(stage + VOFF);
+        u32x4 ones[NK][2];
 #pragma unroll
         for (int i = 0; i < NK; i++)
 #pragma unroll
-          for (int t = 0; t < 2; t++)
+          for (int h = 0; h < 2; h++)
 #pragma unroll
             for (int j = 0; j < 4; j++)
-              pt[i][t][j] = (masked(k, i, 8 * t + 2 * j) ? 0u : kOne) | (masked(k, i, 8 * t + 2 * j + 1) ? 0u : kOne << 16);
+              ones[i][h][j] = (masked(k, i, 8 * h + 2 * j) ? 0u : kOne) | (masked(k, i, 8 * h + 2 * j + 1) ? 0u : kOne << 16);
 #pragma unroll
         for (int c = 0; c < DT; c++) {
           v16f n = {0};
 #pragma unroll
           for (int i = 0; i < NK; i++)
 #pragma unroll
-            for (int t = 0; t < 2; t++) n = mfma32<VBF>(values_of(stage, i, t, c), pt[i][t], n);
+            for (int h = 0; h < 2; h++) n = mfma32<VBF>(values_of(stage, i, h, c), ones[i][h], n);
 #pragma unroll
           for (int v = 0; v < 16; v++) o[c][v] = n[v] > 0.0f ? NAN : o[c][v];
         }
       }
     }
-    if (more) widen(STAGE - stage);
-    stage = STAGE - stage;
+    if (here) products(stage + VOFF);
+    done();
   }
 
   // ---- results
@@ -555,12 +596,12 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   }
 }
 
-template <int D, int BITS, bool BF16, bool EXT>
+template <int D, int BITS, bool BF16, bool EXT, bool FINE>
 hipError_t go_prompt(const PromptArgs &a, hipStream_t s) {
   const int bytes = prompt_lds_bytes(D, BITS);
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(prompt_kernel<D, BITS, BF16, EXT>), bytes);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(prompt_kernel<D, BITS, BF16, EXT, FINE>), bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((prompt_kernel<D, BITS, BF16, EXT>), dim3((uint32_t)a.blocks), dim3(kPromptThreads), bytes, s, a);
+  hipLaunchKernelGGL((prompt_kernel<D, BITS, BF16, EXT, FINE>), dim3((uint32_t)a.blocks), dim3(kPromptThreads), bytes, s, a);
   return hipGetLastError();
 }
 
@@ -569,12 +610,16 @@ hipError_t go_prompt(const PromptArgs &a, hipStream_t s) {
 // one head size's kernels (a file each)
 template <int D>
 hipError_t launch_prompt_d(const PromptArgs &a, bool bf16, hipStream_t s) {
+  typedef std::true_type Yes;
+  typedef std::false_type No;
   const bool ext = a.cap > 0.0f || a.slopes != nullptr;
-  auto go = [&](auto bits, auto b) -> hipError_t {
-    return ext ? go_prompt<D, decltype(bits)::value, decltype(b)::value, true>(a, s)
-               : go_prompt<D, decltype(bits)::value, decltype(b)::value, false>(a, s);
+  auto go = [&](auto bits, auto b, auto e) -> hipError_t {
+    constexpr int BITS = decltype(bits)::value;
+    constexpr bool BF16 = decltype(b)::value, EXT = decltype(e)::value;
+    return a.fine ? go_prompt<D, BITS, BF16, EXT, true>(a, s) : go_prompt<D, BITS, BF16, EXT, false>(a, s);
   };
-  auto go_type = [&](auto bits) -> hipError_t { return bf16 ? go(bits, std::true_type()) : go(bits, std::false_type()); };
+  auto go_ext = [&](auto bits, auto b) -> hipError_t { return ext ? go(bits, b, Yes()) : go(bits, b, No()); };
+  auto go_type = [&](auto bits) -> hipError_t { return bf16 ? go_ext(bits, Yes()) : go_ext(bits, No()); };
   if (a.c.bits == 16) return go_type(std::integral_constant<int, 16>());
   if (a.c.bits == 8) return go_type(std::integral_constant<int, 8>());
   return go_type(std::integral_constant<int, 4>());
