@@ -89,10 +89,11 @@ class Block:
     def prompt(self, x, positions, slots, starts, page_table, lengths):
         """x [tokens, hidden]: new tokens of streams, one stream after the other from rows
         `starts` on, the last of each stream's `lengths`: written to the cache, and
-        attended to as the cache holds them."""
+        attended to as the cache holds them.  (Exact attention: the layers' 4-bit quantizer
+        turns last bits into steps of codes, and a token is to get here what it gets alone.)"""
         q, k, v = self.heads_of(x)
         q = tq.qk_norm_rope_append(self.cache, q, k, v, positions, self.rope, slots, self.q_norm, self.k_norm)
-        return self.rest(x, tq.prompt_attention(self.cache, q, starts, page_table, lengths))
+        return self.rest(x, tq.prompt_attention(self.cache, q, starts, page_table, lengths, exact=True))
 
     def decode(self, x, positions, slots, page_table, lengths, pages=None):
         """x [streams, hidden]: one new token of every stream, at `positions` and in
@@ -102,7 +103,7 @@ class Block:
         if pages is None:
             return self.rest(x, tq.paged_attention(self.cache, q, page_table, lengths))
         return self.rest(x, tq.shared_prefix_attention(self.cache, q, pages.members, pages.prefix, pages.prefix_lengths,
-                                                       page_table, lengths))
+                                                       page_table, lengths, exact=True))
 
 
 def captured(block, *tensors):

@@ -426,11 +426,14 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
 /* How a score is made of a query q at position p and the key k at position j:
  *   s = scale * (q . k);  softcap > 0: s = softcap * tanh(s / softcap);
  *   slopes != NULL: s -= slopes[query head] * |p - j|  (fp32 [q_heads]).
- * window > 0: only keys j > p - window. */
+ * window > 0: only keys j > p - window.
+ * exact: the softmax's weights enter the product with v as two 16-bit terms, 22 bits (16-bit
+ * cache of bf16 values: 16), and not rounded once; about 30 % more time where the products
+ * bound it.  (tq_paged_attention holds that much in any case.) */
 typedef struct {
     float scale, softcap;
     const float *slopes;
-    int32_t window;
+    int32_t window, exact;
 } tq_scores;
 
 /* tq_paged_attention with such scores, the token at position lengths[i] - 1 (its scratch
@@ -464,7 +467,7 @@ tq_status tq_paged_attention_scored(const tq_kv_cache *c, const tq_head_rows *q,
  * What a row does not see (NaN too) has no effect on it; a value that is not finite leaves its
  * channel NaN or infinite in the rows that see it (8 and 4 bits: a scale that is NaN, all
  * channels).  Scores, softmax and sums are fp32; a weight enters the product with v rounded
- * once, to 11 bits (16-bit cache of bf16 values: 8), the divisor and the log-sum-exp take it
+ * once, to 11 bits (16-bit cache of bf16 values: 8), unless exact; the divisor and the log-sum-exp take it
  * unrounded.  One launch, or two where the keys of a row are split; the result does not depend
  * on timing.  tokens == 0 is a no-op; batch from 1 to 65535 (0 with tokens == 0), max_pages *
  * page_size <= 2^30, tokens * q_heads < 2^31, (tokens * q_heads + 128 * batch * kv_heads) / 128 < 2^24.

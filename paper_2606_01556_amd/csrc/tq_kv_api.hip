@@ -225,7 +225,7 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
                              int q_heads, const int32_t *page_table, int64_t table_stride, int max_pages,
                              const int32_t *lengths, float scale, int window, void *out, float *lse,
                              void *scratch, void *stream) {
-  const tq_scores scores = {scale, 0.0f, nullptr, window};
+  const tq_scores scores = {scale, 0.0f, nullptr, window, 1};
   return attend(c, q, dtype, batch, q_heads, page_table, table_stride, max_pages, lengths, &scores, out, lse, scratch, stream);
 }
 
@@ -278,6 +278,7 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
   a.table = page_table; a.table_stride = table_stride; a.max_pages = max_pages;
   a.lengths = lengths; a.prefix = prefix; a.first = first;
   a.scale = scores->scale; a.cap = scores->softcap; a.slopes = scores->slopes; a.window = scores->window;
+  a.fine = scores->exact != 0;
   a.out = static_cast<uint16_t *>(out);
   a.lse = lse;
   a.scratch = static_cast<float *>(scratch);
@@ -341,6 +342,7 @@ tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q
   x.lengths = prefix_lengths; x.own = lengths; x.own_most = max_pages * c->page_size;
   x.scale = scores->scale; x.cap = scores->softcap; x.slopes = scores->slopes;
   x.shared = true;
+  x.fine = scores->exact != 0;
   x.out = static_cast<uint16_t *>(out);
   x.lse = lse;
   x.scratch = static_cast<float *>(scratch);

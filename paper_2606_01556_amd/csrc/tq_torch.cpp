@@ -398,9 +398,9 @@ PyObject *attend(PyObject *const *a, Py_ssize_t) {
 }
 
 // prefix(cache, q, members, prefix_table, prefix_lengths, page_table, lengths, scale or None, softcap, slopes or None,
-//        return_lse, device, stream): out or (out, lse)
+//        exact, return_lse, device, stream): out or (out, lse)
 PyObject *prefix(PyObject *const *a, Py_ssize_t) {
-  const int64_t dev = to_int(a[11]);
+  const int64_t dev = to_int(a[12]);
   const Cache &c = cache_of(a[0], dev);
   tq_head_rows q;
   const at::Tensor &qt = queries(a[1], c, dev, q);
@@ -415,8 +415,9 @@ PyObject *prefix(PyObject *const *a, Py_ssize_t) {
   const int32_t *prefix_lengths = static_cast<const int32_t *>(plain(a[4], "prefix_lengths", at::kInt, {groups}, dev));
   const int32_t *table = page_table_of(a[5], "page_table", batch, dev, pages, stride);
   const int32_t *lengths = static_cast<const int32_t *>(plain(a[6], "lengths", at::kInt, {batch}, dev));
-  const tq_scores s = scores_of(a[7], nullptr, a[8], a[9], hq, c.c.head_dim, dev);
-  const bool return_lse = to_bool(a[10]);
+  tq_scores s = scores_of(a[7], nullptr, a[8], a[9], hq, c.c.head_dim, dev);
+  s.exact = to_bool(a[10]);
+  const bool return_lse = to_bool(a[11]);
   const size_t bytes = L.prefix_bytes(&c.c, batch, hq, groups, prefix_pages, pages);
   const at::Tensor out = fresh({batch, hq, c.c.head_dim}, qt.scalar_type(), dev);
   at::Tensor lse, scratch;
@@ -426,15 +427,15 @@ PyObject *prefix(PyObject *const *a, Py_ssize_t) {
     check(L.prefix(&c.c, &q, dtype_of(qt.scalar_type()), batch, hq, groups, members, prefix_table, prefix_stride, prefix_pages,
                    prefix_lengths, table, stride, pages, lengths, &s, out.data_ptr(),
                    return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr, bytes > 0 ? scratch.data_ptr() : nullptr,
-                   to_stream(a[12])),
+                   to_stream(a[13])),
           "tq_shared_prefix_attention");
   return return_lse ? wrap2(out, lse) : wrap(out);
 }
 
 // prompt(cache, q, starts, page_table, lengths, scale or None, window, prefix or None, first or None, softcap,
-//        slopes or None, return_lse, device, stream): out or (out, lse)
+//        slopes or None, exact, return_lse, device, stream): out or (out, lse)
 PyObject *prompt(PyObject *const *a, Py_ssize_t) {
-  const int64_t dev = to_int(a[12]);
+  const int64_t dev = to_int(a[13]);
   const Cache &c = cache_of(a[0], dev);
   tq_head_rows q;
   const at::Tensor &qt = queries(a[1], c, dev, q);
@@ -449,8 +450,9 @@ PyObject *prompt(PyObject *const *a, Py_ssize_t) {
   const int32_t *lengths = static_cast<const int32_t *>(plain(a[4], "lengths", at::kInt, {batch}, dev));
   const int32_t *prefix = static_cast<const int32_t *>(plain_or_null(a[7], "prefix", at::kInt, {batch}, dev));
   const int32_t *first = static_cast<const int32_t *>(plain_or_null(a[8], "first", at::kInt, {tokens}, dev));
-  const tq_scores s = scores_of(a[5], a[6], a[9], a[10], hq, c.c.head_dim, dev);
-  const bool return_lse = to_bool(a[11]);
+  tq_scores s = scores_of(a[5], a[6], a[9], a[10], hq, c.c.head_dim, dev);
+  s.exact = to_bool(a[11]);
+  const bool return_lse = to_bool(a[12]);
   const size_t bytes = L.prompt_bytes(&c.c, tokens, batch, hq, pages, s.window);
   const at::Tensor out = fresh({tokens, hq, c.c.head_dim}, qt.scalar_type(), dev);
   at::Tensor lse, scratch;
@@ -459,7 +461,7 @@ PyObject *prompt(PyObject *const *a, Py_ssize_t) {
   if (tokens > 0)
     check(L.prompt(&c.c, &q, dtype_of(qt.scalar_type()), tokens, batch, hq, starts, table, stride, pages, lengths, prefix, first,
                    &s, out.data_ptr(), return_lse ? static_cast<float *>(lse.data_ptr()) : nullptr,
-                   bytes > 0 ? scratch.data_ptr() : nullptr, to_stream(a[13])),
+                   bytes > 0 ? scratch.data_ptr() : nullptr, to_stream(a[14])),
           "tq_prompt_attention");
   return return_lse ? wrap2(out, lse) : wrap(out);
 }
@@ -559,7 +561,7 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 #define TQ_METHOD(name, n) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void *>(entry<name, n>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {TQ_METHOD(bind, 13), TQ_METHOD(make_cache, 4), TQ_METHOD(append, 6), TQ_METHOD(read, 5),
-                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 11), TQ_METHOD(prompt, 14), TQ_METHOD(prefix, 13), TQ_METHOD(add_norm, 10),
+                         TQ_METHOD(norm_rope, 10), TQ_METHOD(norm_rope_append, 14), TQ_METHOD(attend, 11), TQ_METHOD(prompt, 15), TQ_METHOD(prefix, 14), TQ_METHOD(add_norm, 10),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tqtorch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

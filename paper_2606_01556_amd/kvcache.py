@@ -48,7 +48,7 @@ class _NormRope(ctypes.Structure):      # tq_norm_rope
 
 class _Scores(ctypes.Structure):        # tq_scores
     _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p),
-                ("window", ctypes.c_int32)]
+                ("window", ctypes.c_int32), ("exact", ctypes.c_int32)]
 
 
 class _ResidualNorm(ctypes.Structure):  # tq_residual_norm
@@ -273,7 +273,8 @@ def paged_attention(cache: KVCache, q, page_table, lengths, scale: float | None 
 
 
 def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: float | None = None, window: int = 0,
-                     prefix=None, first=None, softcap: float = 0.0, slopes=None, return_lse: bool = False, stream=None):
+                     prefix=None, first=None, softcap: float = 0.0, slopes=None, exact: bool = False,
+                     return_lse: bool = False, stream=None):
     """Attention of many new tokens of every stream over the cache, which holds them
     already (tq_prompt_attention): prompts, chunks of prompts, tokens to verify.  q
     [tokens, q_heads, head_dim] holds the streams' new tokens one stream after the other,
@@ -284,7 +285,10 @@ def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: floa
     with prefix [batch] int32 also all of its stream's first prefix[i] tokens; with first
     [tokens] int32 nothing before position first[r] (where its document starts).  softcap
     > 0: scores s become softcap * tanh(s / softcap); slopes [q_heads] float32: less
-    slopes[h] times the distance.  scale: head_dim^-1/2 by default.
+    slopes[h] times the distance.  scale: head_dim^-1/2 by default.  The softmax's weights
+    enter the product with v rounded to 16 bits; exact: with 22 bits (16-bit cache of
+    bfloat16: 16) as in ``paged_attention``, in about 30 % more time, for a token's result
+    not to depend on whether it came in a prompt or alone by more than its last rounding.
 
     Returns out [tokens, q_heads, head_dim] of q's type, zeros for a token that sees
     nothing and for rows of no stream; with return_lse (out, lse [tokens, q_heads]
@@ -293,14 +297,14 @@ def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: floa
     if stream is not None:
         return _elsewhere(stream, (q, starts, page_table, lengths, prefix, first, slopes, *cache._t),
                           lambda dev, st: _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first,
-                                                         softcap, slopes, return_lse, dev, st))
-    return _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first, softcap, slopes, return_lse,
-                          *_here())
+                                                         softcap, slopes, exact, return_lse, dev, st))
+    return _native.prompt(c, q, starts, page_table, lengths, scale, window, prefix, first, softcap, slopes, exact,
+                          return_lse, *_here())
 
 
 def shared_prefix_attention(cache: KVCache, q, members, prefix_table, prefix_lengths, page_table, lengths,
-                            scale: float | None = None, softcap: float = 0.0, slopes=None, return_lse: bool = False,
-                            stream=None):
+                            scale: float | None = None, softcap: float = 0.0, slopes=None, exact: bool = False,
+                            return_lse: bool = False, stream=None):
     """Attention of one new token of every stream, q [batch, q_heads, head_dim], over a
     prefix that its group shares, read once for the group, and over the stream's own
     tokens behind it (tq_shared_prefix_attention).  Group g's streams are rows members[g]
@@ -308,7 +312,7 @@ def shared_prefix_attention(cache: KVCache, q, members, prefix_table, prefix_len
     prefix the first prefix_lengths[g] tokens of the pages prefix_table[g] (prefix_table
     [groups, prefix_pages] int32).  page_table and lengths: the streams' own tokens, the
     newest among them, as in ``paged_attention``; scale, softcap and slopes as there, with
-    distances across the prefix.
+    distances across the prefix; exact as in ``prompt_attention``, for the prefix's keys.
 
     Returns out [batch, q_heads, head_dim] of q's type, zeros for a stream without prefix
     and tokens; with return_lse (out, lse [batch, q_heads] float32)."""
@@ -316,9 +320,9 @@ def shared_prefix_attention(cache: KVCache, q, members, prefix_table, prefix_len
     if stream is not None:
         return _elsewhere(stream, (q, members, prefix_table, prefix_lengths, page_table, lengths, slopes, *cache._t),
                           lambda dev, st: _native.prefix(c, q, members, prefix_table, prefix_lengths, page_table, lengths,
-                                                         scale, softcap, slopes, return_lse, dev, st))
+                                                         scale, softcap, slopes, exact, return_lse, dev, st))
     return _native.prefix(c, q, members, prefix_table, prefix_lengths, page_table, lengths, scale, softcap, slopes,
-                          return_lse, *_here())
+                          exact, return_lse, *_here())
 
 
 def add_rms_norm(x, residual=None, weight=None, post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6,

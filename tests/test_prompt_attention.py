@@ -7,7 +7,7 @@ bf16, relative to the result's binade at most).  For weights w that sum to 1 and
   u |o|                          the one rounding of the result
   sum_j w_j |v_j| (p + e_j + ē)  p: the one rounding of a weight, 2^-11 where they enter the
                                  second product in fp16 (all caches but bf16 rows), 2^-8 in
-                                 bf16; e_j: what a score may be off by, ē its mean over w (the
+                                 bf16, and with two terms (exact) the squares of these; e_j: what a score may be off by, ē its mean over w (the
                                  divisor's share).  e_j = 2^-19 of scale sum |q k| (products and
                                  sums of up to 256 terms in fp32), plus 2^-21 of the cap (an
                                  exponential and a reciprocal of an ulp or two each), plus 2^-22
@@ -45,7 +45,7 @@ class Prompts(Streams):
         self.new = new
         self.starts = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
 
-    def plain(self, q, scale, window=0, prefix=None, first=None, softcap=0.0, slopes=None):
+    def plain(self, q, scale, window=0, prefix=None, first=None, softcap=0.0, slopes=None, exact=False):
         rows, hq, d = q.shape
         heads = self.k.shape[1]
         wide = not (self.cache.bits == 16 and self.cache.k.dtype == BF16)
@@ -85,7 +85,7 @@ class Prompts(Streams):
                 w = w / safe[:, None]
                 o = w @ vh
                 mean = (w * e).sum(-1)
-                weight = 2.0 ** -11 if wide else 2.0 ** -8
+                weight = (2.0 ** -11 if wide else 2.0 ** -8) ** (2 if exact else 1)
                 off = (w * (weight + e + mean[:, None])) @ np.abs(vh)
                 top = (np.where(seen[:, :, None], np.abs(vh)[None], 0.0).max((0, 1)) if n * t * d < 2 ** 24 else np.abs(vh).max(0))
                 out[r0:r0 + t, h] = o
@@ -121,7 +121,7 @@ def prompts(lens, new, heads, group, d, page, kind, dtype, seed=0, pad=0, scale=
 
 # ------------------------------------------------------------------ refusals, on the CPU
 def scores(**over):
-    s = dict(scale=1.0, softcap=0.0, slopes=None, window=0)
+    s = dict(scale=1.0, softcap=0.0, slopes=None, window=0, exact=0)
     s.update(over)
     return tq.kvcache._Scores(*s.values())
 
@@ -222,6 +222,22 @@ def test_split_keys(kind, dtype, d, lens, new):
                                                       s.table.shape[1], 0) > 0
     held(s, q)
     held(s, q, window=1000, softcap=25.0)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("lens,new", [([1, 90, 333], [1, 90, 20]), ([5000, 40], [3, 1])])
+def test_exact(kind, dtype, d, lens, new):
+    say("exact", kind, dtype, d, lens)
+    s, q = prompts(lens, new, 2, 4, d, 16, kind, dtype)
+    got = held(s, q, exact=True)
+    held(s, q, exact=True, window=70, softcap=9.0)
+    # and so what one token gets by itself, but for the last rounding of each
+    last = s.starts[1:] - 1
+    alone, _, bound, _ = s.plain(q, d ** -0.5, exact=True)
+    one = tq.paged_attention(s.cache, q[torch.from_numpy(last.astype(np.int64))].cuda(), *s.args()).cpu().double().numpy()
+    assert (np.abs(got[last] - one) <= 2 * bound[last]).all()
 
 
 @gpu

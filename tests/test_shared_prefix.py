@@ -130,6 +130,7 @@ def test_shared_prefix(kind, dtype, d, shape):
         s = Shared(*SHARED[shape], heads, d, 16, kind, dtype)
         q = (1.3 * randn(len(s.own), heads * group, d, seed=9)).to(dtype)
         check(*s.call(q, return_lse=True), *s.plain(q, d ** -0.5))
+        check(*s.call(q, return_lse=True, exact=True), *s.plain(q, d ** -0.5, exact=True))
 
 
 @gpu
