@@ -48,51 +48,57 @@ class Prompts(Streams):
     def plain(self, q, scale, window=0, prefix=None, first=None, softcap=0.0, slopes=None, exact=False):
         rows, hq, d = q.shape
         heads = self.k.shape[1]
+        group = hq // heads
+        on = lambda x: torch.as_tensor(np.asarray(x)).cuda()
         wide = not (self.cache.bits == 16 and self.cache.k.dtype == BF16)
-        out, lse = np.zeros((rows, hq, d)), np.full((rows, hq), -np.inf)
-        bound, lse_bound = np.zeros((rows, hq, d)), np.zeros((rows, hq))
+        weight = (2.0 ** -11 if wide else 2.0 ** -8) ** (2 if exact else 1)
+        new = lambda *shape: torch.zeros(shape, dtype=torch.float64, device="cuda")
+        out, lse, bound, lse_bound = new(rows, hq, d), new(rows, hq) - math.inf, new(rows, hq, d), new(rows, hq)
         at = 0
         for i, (n, t) in enumerate(zip(self.lens, self.new)):
             k, v = self.k[at:at + n], self.v[at:at + n]
             at += n
-            r0 = self.starts[i]
+            r = slice(int(self.starts[i]), int(self.starts[i]) + t)
             if n == 0 or t == 0:
                 continue
-            p, j = n - t + np.arange(t)[:, None], np.arange(n)[None]
+            p, j = n - t + torch.arange(t, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
             seen = j <= p
             if prefix is not None:
-                seen = seen | (j < prefix[i])
+                seen = seen | (j < int(prefix[i]))
             if window:
                 seen = seen & (j > p - window)
             if first is not None:
-                seen = seen & (j >= np.asarray(first)[r0:r0 + t, None])
+                seen = seen & (j >= on(first)[r][:, None])
+            # [heads, tokens * group, ...]: a kv head's rows
+            kh, vh = (on(x).double().transpose(0, 1).contiguous() for x in (k, v))
+            x = q[r].cuda().double().view(t, heads, group, d).transpose(0, 1).reshape(heads, -1, d)
+            seen = seen.repeat_interleave(group, 0)[None]
+            s = torch.matmul(x, kh.transpose(1, 2).contiguous()) * scale
+            e = 2.0 ** -19 * torch.matmul(x.abs(), kh.abs().transpose(1, 2).contiguous()) * abs(scale)
+            if softcap:
+                s = softcap * torch.tanh(s / softcap)
+                e = e.clamp(max=2 * softcap) + 2.0 ** -21 * softcap
+            if slopes is not None:
+                slope = torch.as_tensor(np.asarray(slopes)).double().cuda().view(heads, 1, group).expand(-1, t, -1).reshape(heads, -1, 1)
+                s = s - slope * (p - j).abs().repeat_interleave(group, 0)[None]
+            e = e + 2.0 ** -22 * s.abs() + (2.0 ** -18 if self.cache.bits < 16 else 0.0)
+            s = torch.where(seen, s, -math.inf)
             any_seen = seen.any(-1)
-            for h in range(hq):
-                kh, vh, qh = k[:, h * heads // hq], v[:, h * heads // hq], q[r0:r0 + t, h].double().numpy()
-                s = qh @ kh.T * scale
-                e = 2.0 ** -19 * (np.abs(qh) @ np.abs(kh).T) * abs(scale)
-                if softcap:
-                    s = softcap * np.tanh(s / softcap)
-                    e = np.minimum(e, 2 * softcap) + 2.0 ** -21 * softcap
-                if slopes is not None:
-                    s = s - float(slopes[h]) * np.abs(p - j)
-                e = e + 2.0 ** -22 * np.abs(s) + (2.0 ** -18 if self.cache.bits < 16 else 0.0)
-                s = np.where(seen, s, -np.inf)
-                m = np.where(any_seen, s.max(-1, initial=-np.inf), 0.0)
-                w = np.exp(s - m[:, None])
-                total = w.sum(-1)
-                safe = np.where(any_seen, total, 1.0)
-                w = w / safe[:, None]
-                o = w @ vh
-                mean = (w * e).sum(-1)
-                weight = (2.0 ** -11 if wide else 2.0 ** -8) ** (2 if exact else 1)
-                off = (w * (weight + e + mean[:, None])) @ np.abs(vh)
-                top = (np.where(seen[:, :, None], np.abs(vh)[None], 0.0).max((0, 1)) if n * t * d < 2 ** 24 else np.abs(vh).max(0))
-                out[r0:r0 + t, h] = o
-                bound[r0:r0 + t, h] = ulp(q.dtype) * np.abs(o) + off + n * 2.0 ** -36 * top + self.floor
-                lse[r0:r0 + t, h] = np.where(any_seen, m + np.log(safe), -np.inf)
-                lse_bound[r0:r0 + t, h] = mean + 2.0 ** -18 * (1 + np.abs(np.where(any_seen, lse[r0:r0 + t, h], 0.0)))
-        return out, lse, bound, lse_bound
+            m = torch.where(any_seen, s.amax(-1), 0.0)
+            w = torch.exp(s - m[..., None])
+            total = torch.where(any_seen, w.sum(-1), 1.0)
+            w = w / total[..., None]
+            e = torch.where(w > 0, e, 0.0)
+            o = torch.matmul(w, vh)
+            mean = (w * e).sum(-1)
+            off = torch.matmul(w * (weight + e + mean[..., None]), vh.abs())
+            top = vh.abs().amax(1, keepdim=True)
+            b = ulp(q.dtype) * o.abs() + off + n * 2.0 ** -36 * top + self.floor
+            l = torch.where(any_seen, m + torch.log(total), 0.0)
+            back = lambda y: y.view(heads, t, group, *y.shape[2:]).transpose(0, 1).reshape(t, hq, *y.shape[2:])
+            out[r], bound[r] = back(o), back(b)
+            lse[r], lse_bound[r] = back(torch.where(any_seen, l, -math.inf)), back(mean + 2.0 ** -18 * (1 + l.abs()))
+        return [y.cpu().numpy() for y in (out, lse, bound, lse_bound)]
 
     def call(self, q, **kw):
         cuda = lambda x, t=torch.int32: None if x is None else torch.as_tensor(np.asarray(x)).to(t).cuda()
