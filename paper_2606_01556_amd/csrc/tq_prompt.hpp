@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
 
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
   int *const bounds = reinterpret_cast<int *>(smem + 2 * STAGE), *const flag = bounds + 4 * W;
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
 
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const int r32 = lane & 31, half = lane >> 5;
@@ -230,92 +230,90 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   for (int i = 0; i < DT; i++) o[i] = v16f{0};
   float m = -FLT_MAX, l = 0.0f;      // (finite: keys whose score is -infinity have the weight 0 also before the first other one)
 
-  // ---- loads.  A wavefront's load takes rows of one page (up to 16 rows); keys outside the
+  // ---- loads.  A wavefront takes 16 rows of a tile, which lie in one page; keys outside the
   // rows' intervals take the nearest one's row.
   const_i32 *const pages = (const_i32 *)(a.table + s * a.table_stride);
   auto held = [&](int key) -> int { return min(max(key, all_lo), all_hi - 1); };
   constexpr int PIECE = BITS == 16 ? 16 : KT * RB / T < 16 ? KT * RB / T : 16;    // bytes of a lane's load
-  constexpr int PR = RB / PIECE, LR = 64 / PR, NL = KT / (LR * W);                // lanes of a row, rows of a load, loads
-  static_assert(LR <= 16 && NL >= 1 && NL * LR * W == KT);
+  constexpr int PR = RB / PIECE, LR = 64 / PR, NL = 16 / LR;                      // lanes of a row, rows of a load, loads
+  static_assert(LR <= 16 && NL * LR == 16 && 16 * W == KT);
   const int lrow = lane / PR, lpiece = lane % PR;
-  int page[NL];
-  auto load_pages = [&](int k) {
-#pragma unroll
-    for (int i = 0; i < NL; i++) page[i] = pages[held(k + (i * W + w) * LR) >> lps];
-  };
-  // byte offset of a load's page, from this kv head's rows of page 0
+  const uint32_t in_page = (1u << lps) - 1;
+  int page;
+  auto load_page = [&](int k) { page = pages[held(k + 16 * w) >> lps]; };
   const uint32_t page_rows = (uint32_t)hkv << lps;                // <= 2^25 (host)
-  const uint8_t *const kbase = a.c.k + ((int64_t)kvh << lps) * RB, *const vbase = a.c.v + ((int64_t)kvh << lps) * RB;
-  auto base_of = [&](int i) -> int64_t { return (int64_t)((uint64_t)(uint32_t)min(max(page[i], 0), a.c.pages - 1) * page_rows * RB); };
+  const int64_t first_row = (int64_t)kvh << lps;
+  auto swizzle = [](int r, bool value) -> int { return value ? (LC > 8 ? 2 * (r & 7) : 2 * (r & 3)) : (LC > 8 ? r & 15 : r & 7); };
   u32x4 kraw[BITS < 16 ? NL : 1], vraw[BITS < 16 ? NL : 1];       // codes on their way
   uint16_t sraw = 0;
-  auto load = [&](int k, uint32_t stage) {
+  // inside: all keys of the tile lie between the intervals' ends
+  auto load = [&](int k, uint32_t stage, auto inside) {
+    constexpr bool INSIDE = decltype(inside)::value;
+    const int k16 = k + 16 * w;
+    int64_t rows = (int64_t)((uint64_t)(uint32_t)min(max(page, 0), a.c.pages - 1) * page_rows) + first_row;
+    if constexpr (INSIDE) rows += (uint32_t)k16 & in_page;
+    auto row_of = [&](int r) -> uint32_t { return INSIDE ? (uint32_t)r : (uint32_t)held(k16 + r) & in_page; };
+    const uint8_t *const kp = a.c.k + rows * RB, *const vp = a.c.v + rows * RB;
 #pragma unroll
     for (int i = 0; i < NL; i++) {
-      const int64_t base = base_of(i);
-      const int r = (i * W + w) * LR + lrow;
-      const uint32_t off = (uint32_t)(held(k + r) & ((1 << lps) - 1)) * RB;
+      const int r = i * LR + lrow;
+      const uint32_t off = row_of(r) * RB;
       if constexpr (BITS == 16) {
-        const uint32_t to = stage + (i * W + w) * 1024;
-        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? r & 15 : r & 7)), kbase + base, lds0 + to);
-        load_to_lds(off + 16 * (lpiece ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3))), vbase + base, lds0 + to + VOFF);
+        const uint32_t to = lds0 + stage + w * 16 * LB + i * 1024;
+        load_to_lds(off + 16 * (lpiece ^ swizzle(r, false)), kp, to);
+        load_to_lds(off + 16 * (lpiece ^ swizzle(r, true)), vp, to + VOFF);
       } else if constexpr (PIECE == 16) {
-        kraw[i] = *reinterpret_cast<const u32x4 *>(kbase + base + off + 16 * lpiece);
-        vraw[i] = *reinterpret_cast<const u32x4 *>(vbase + base + off + 16 * lpiece);
+        kraw[i] = *reinterpret_cast<const u32x4 *>(kp + off + 16 * lpiece);
+        vraw[i] = *reinterpret_cast<const u32x4 *>(vp + off + 16 * lpiece);
       } else {
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(kbase + base + off + 8 * lpiece);
-        const u32x2 y = *reinterpret_cast<const u32x2 *>(vbase + base + off + 8 * lpiece);
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(kp + off + 8 * lpiece);
+        const u32x2 y = *reinterpret_cast<const u32x2 *>(vp + off + 8 * lpiece);
         kraw[i] = u32x4{x.x, x.y, 0, 0};
         vraw[i] = u32x4{y.x, y.y, 0, 0};
       }
     }
-    if constexpr (BITS < 16) {
-      // (wavefront 0 the keys' scales, 1 the values')
-      if (w < 2) {
-        const int key = held(k + lane);
-        const int64_t p = min(max(pages[key >> lps], 0), a.c.pages - 1);
-        sraw = (w == 0 ? a.c.ks : a.c.vs)[((p * hkv + kvh) << lps) + (key & ((1 << lps) - 1))];
-      }
-    }
+    // (lanes 0 to 15 the keys' scales, 16 to 31 the values')
+    if constexpr (BITS < 16)
+      if (lane < 32) sraw = (lane < 16 ? a.c.ks : a.c.vs)[rows + row_of(lane & 15)];
   };
   // codes as 16-bit values in LDS: keys in Q's type, values in fp16
   auto widen = [&](uint32_t stage) {
     if constexpr (BITS < 16) {
       constexpr int WORDS = PIECE / 4, PER = BITS == 8 ? 2 : 1;   // words of a piece, words of 8 codes
 #pragma unroll
-      for (int i = 0; i < NL; i++) {
-        const int r = (i * W + w) * LR + lrow;
+      for (int i = 0; i < 2 * NL; i++) {
+        const bool value = i >= NL;
+        const int r = 16 * w + i % NL * LR + lrow;
+        const u32x4 raw = value ? vraw[i % NL] : kraw[i % NL];
 #pragma unroll
         for (int e = 0; e < WORDS / PER; e++) {
-          const int c = lpiece * (WORDS / PER) + e;
-          auto eight = [&](const u32x4 &raw, auto bf) -> u32x4 {
-            constexpr bool TO = decltype(bf)::value;
-            uint32_t w0, w1, y0, y1, y2, y3;
-            if constexpr (BITS == 8) { w0 = raw[2 * e]; w1 = raw[2 * e + 1]; }
-            else tq4_to_fp8(raw[e], w0, w1);
-            widen4<TO>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
-            widen4<TO>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
-            return u32x4{y0, y1, y2, y3};
-          };
-          *reinterpret_cast<u32x4 *>(smem + stage + r * LB + 16 * (c ^ (LC > 8 ? r & 15 : r & 7))) =
-              eight(kraw[i], std::integral_constant<bool, BF16>());
-          *reinterpret_cast<u32x4 *>(smem + stage + VOFF + r * LB + 16 * (c ^ (LC > 8 ? 2 * (r & 7) : 2 * (r & 3)))) =
-              eight(vraw[i], std::integral_constant<bool, false>());
+          uint32_t w0, w1, y0, y1, y2, y3;
+          if constexpr (BITS == 8) { w0 = raw[2 * e]; w1 = raw[2 * e + 1]; }
+          else tq4_to_fp8(raw[e], w0, w1);
+          if (BF16 && !value) {
+            widen4<true>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+            widen4<true>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+          } else {
+            widen4<false>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+            widen4<false>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+          }
+          *reinterpret_cast<u32x4 *>(smem + stage + (value ? VOFF : 0) + r * LB + 16 * ((lpiece * (WORDS / PER) + e) ^ swizzle(r, value))) =
+              u32x4{y0, y1, y2, y3};
         }
       }
-      // the keys' scales; the values' as binades and their inverse.  (A value scale of zero, whose
+      // The keys' scales; the values' as binades and their inverse.  (A value scale of zero, whose
       // codes are zero, counts as fp16's smallest, and so does NaN, whose row is marked.)
-      float *const to = reinterpret_cast<float *>(smem + stage + SOFF) + lane;
+      float *const to = reinterpret_cast<float *>(smem + stage + SOFF) + 16 * w + (lane & 15);
       const float x = half_bits_to_float(sraw);
-      if (w == 0) {
+      if (lane < 16) {
         to[0] = x;
-      } else if (w == 1) {
+      } else if (lane < 32) {
         const float y = fmaxf(x, kLeastScale);
         to[KT] = __builtin_amdgcn_logf(y);
         to[2 * KT] = 1.0f / y;
-        const uint64_t nan = __ballot(x != x);
-        if (lane == 0) *reinterpret_cast<uint64_t *>(smem + stage + SOFF + 12 * KT) = nan;
       }
+      const uint64_t nan = __ballot(x != x);
+      if (lane == 0) reinterpret_cast<uint16_t *>(smem + stage + SOFF + 12 * KT)[w] = (uint16_t)(nan >> 16);
     }
   };
 
@@ -472,19 +470,18 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   const int end = k1 - k0;
   uint32_t stage = 0;
   if (end > 0) {
-    load_pages(tile_at(0));
-    load(tile_at(0), 0);
+    load_page(tile_at(0));
+    load(tile_at(0), 0, std::false_type());
     widen(0);
-    load_pages(tile_at(KT));
+    load_page(tile_at(KT));
   }
   int t = 0;
   // a tile's data is there, and the next one's on its way
   auto next = [&]() {
     wait_all();
-    if (t + KT < end) {
-      load(tile_at(t + KT), STAGE - stage);
-      load_pages(tile_at(t + 2 * KT));
-    }
+    if (t + KT < skip) load(p0 + t + KT, STAGE - stage, std::true_type());
+    else if (t + KT < end) load(tile_at(t + KT), STAGE - stage, std::false_type());
+    load_page(tile_at(t + 2 * KT));
     if constexpr (BITS < 16) {
       // rows whose value scale is NaN read as NaN
       const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + stage + SOFF + 12 * KT);
