@@ -50,11 +50,14 @@ constexpr int kTileKeys = 64;
 constexpr float kTopBinades = 15.99f;      // 2^15.99 < 65504
 
 // wavefronts of a SIMD that the registers are cut for
-constexpr int prompt_occupancy(int d) { return d == 256 ? 1 : d == 128 ? 2 : 3; }
+constexpr int prompt_occupancy(int d, int bits) { return d == 256 ? 1 : d == 128 || bits < 16 ? 2 : 3; }
 
-// bytes of LDS: two stages of keys, values and (codes) their scales; four pairs of bounds and a flag
-constexpr int prompt_stage(int d, int bits) { return kTileKeys * d * 4 + (bits < 16 ? kTileKeys * 12 + 16 : 0); }
-constexpr int prompt_lds_bytes(int d, int bits) { return 2 * prompt_stage(d, bits) + 64 * kPromptWaves; }
+// Bytes of LDS: two tiles of keys, two of values, and (codes) what goes with them: the keys'
+// scales; the values' as binades and inverse, and which of them are NaN.  Then four bounds a
+// wavefront and a flag.
+constexpr int kKeyScales = kTileKeys * 4, kValueScales = kTileKeys * 8 + 16;
+constexpr int prompt_tiles(int d, int bits) { return kTileKeys * d * 8 + (bits < 16 ? 2 * (kKeyScales + kValueScales) : 0); }
+constexpr int prompt_lds_bytes(int d, int bits) { return prompt_tiles(d, bits) + 64 * kPromptWaves; }
 
 template <bool BF16>
 __device__ __forceinline__ v16f mfma32(u32x4 a, u32x4 b, v16f c) {
@@ -67,6 +70,11 @@ __device__ __forceinline__ v16f mfma32(u32x4 a, u32x4 b, v16f c) {
 // 16 bytes per lane from sbase + voff into LDS at lds + 16 * lane
 __device__ __forceinline__ void load_to_lds(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds) : "memory");
+}
+// a wave-uniform pointer, in scalar registers
+__device__ __forceinline__ const uint8_t *uniform_at(const uint8_t *p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const uint8_t *>((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
 }
 // this wavefront's loads and LDS accesses done, then all wavefronts'
 __device__ __forceinline__ void wait_all() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -101,17 +109,21 @@ struct Interval {
 };
 
 template <int D, int BITS, bool BF16, bool EXT, bool FINE>
-__global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_kernel(const PromptArgs a) {
+__global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void prompt_kernel(const PromptArgs a) {
   constexpr int KT = kTileKeys, W = kPromptWaves, T = kPromptThreads;
   constexpr int RB = D * BITS / 8;              // bytes of a cache row
   constexpr int LB = D * 2, LC = LB / 16;       // bytes and 16-byte pieces of a row in LDS
-  constexpr int KS = D / 16, DT = D / 32, NK = KT / 32;
+  constexpr int KS = D / 16, DT = D / 32;
   constexpr bool VBF = BITS == 16 && BF16;      // type of the second product
-  constexpr int VOFF = KT * LB, SOFF = 2 * KT * LB, STAGE = prompt_stage(D, BITS);
+  constexpr int TB = KT * LB;                   // bytes of a tile in LDS
+  constexpr auto key_tile = [](int odd) { return odd * TB; };
+  constexpr auto value_tile = [](int odd) { return (2 + odd) * TB; };
+  constexpr auto key_scales = [](int odd) { return 4 * TB + odd * kKeyScales; };
+  constexpr auto value_scales = [](int odd) { return 4 * TB + 2 * kKeyScales + odd * kValueScales; };
   constexpr uint32_t kOne = VBF ? 0x3f80u : 0x3c00u;
 
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  int *const bounds = reinterpret_cast<int *>(smem + 2 * STAGE), *const flag = bounds + 4 * W;
+  int *const bounds = reinterpret_cast<int *>(smem + prompt_tiles(D, BITS)), *const flag = bounds + 4 * W;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)smem;
 
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
@@ -239,161 +251,139 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   static_assert(LR <= 16 && NL * LR == 16 && 16 * W == KT);
   const int lrow = lane / PR, lpiece = lane % PR;
   const uint32_t in_page = (1u << lps) - 1;
-  int page;
-  auto load_page = [&](int k) { page = pages[held(k + 16 * w) >> lps]; };
+  auto page_of = [&](int k) -> int { return uniform(pages[held(k + 16 * w) >> lps]); };
   const uint32_t page_rows = (uint32_t)hkv << lps;                // <= 2^25 (host)
   const int64_t first_row = (int64_t)kvh << lps;
-  auto swizzle = [](int r, bool value) -> int { return value ? (LC > 8 ? 2 * (r & 7) : 2 * (r & 3)) : (LC > 8 ? r & 15 : r & 7); };
-  u32x4 kraw[BITS < 16 ? NL : 1], vraw[BITS < 16 ? NL : 1];       // codes on their way
-  uint16_t sraw = 0;
-  // inside: all keys of the tile lie between the intervals' ends
-  auto load = [&](int k, uint32_t stage, auto inside) {
+  auto swizzle = [](int r, bool value) -> int { return value ? 4 * (LC > 8 ? r & 3 : r >> 1 & 1) : (LC > 8 ? r & 15 : r >> 1 & 7); };
+  constexpr int NR = BITS < 16 ? NL : 1;
+  u32x4 kraw[NR], vraw[NR];                                       // codes on their way
+  uint16_t kscale = 0, vscale = 0;
+  // The keys or values from k on (in that page) to LDS, or codes to registers.  inside: all of
+  // them lie between the intervals' ends.
+  auto load = [&](auto value, u32x4 (&raw)[NR], uint16_t &scale, int k, int page, uint32_t to, auto inside) __attribute__((always_inline)) {
     constexpr bool INSIDE = decltype(inside)::value;
+    constexpr bool VALUE = decltype(value)::value;
     const int k16 = k + 16 * w;
     int64_t rows = (int64_t)((uint64_t)(uint32_t)min(max(page, 0), a.c.pages - 1) * page_rows) + first_row;
     if constexpr (INSIDE) rows += (uint32_t)k16 & in_page;
-    auto row_of = [&](int r) -> uint32_t { return INSIDE ? (uint32_t)r : (uint32_t)held(k16 + r) & in_page; };
-    const uint8_t *const kp = a.c.k + rows * RB, *const vp = a.c.v + rows * RB;
+    const uint8_t *const p = uniform_at((VALUE ? a.c.v : a.c.k) + rows * RB);
+    auto go = [&](auto row_of) {
 #pragma unroll
-    for (int i = 0; i < NL; i++) {
-      const int r = i * LR + lrow;
-      const uint32_t off = row_of(r) * RB;
-      if constexpr (BITS == 16) {
-        const uint32_t to = lds0 + stage + w * 16 * LB + i * 1024;
-        load_to_lds(off + 16 * (lpiece ^ swizzle(r, false)), kp, to);
-        load_to_lds(off + 16 * (lpiece ^ swizzle(r, true)), vp, to + VOFF);
-      } else if constexpr (PIECE == 16) {
-        kraw[i] = *reinterpret_cast<const u32x4 *>(kp + off + 16 * lpiece);
-        vraw[i] = *reinterpret_cast<const u32x4 *>(vp + off + 16 * lpiece);
-      } else {
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(kp + off + 8 * lpiece);
-        const u32x2 y = *reinterpret_cast<const u32x2 *>(vp + off + 8 * lpiece);
-        kraw[i] = u32x4{x.x, x.y, 0, 0};
-        vraw[i] = u32x4{y.x, y.y, 0, 0};
+      for (int i = 0; i < NL; i++) {
+        const int r = i * LR + lrow;
+        const uint32_t off = row_of(r) * RB;
+        if constexpr (BITS == 16) {
+          load_to_lds(off + 16 * (lpiece ^ swizzle(r, VALUE)), p, lds0 + to + w * 16 * LB + i * 1024);
+        } else if constexpr (PIECE == 16) {
+          raw[i] = *reinterpret_cast<const u32x4 *>(p + off + 16 * lpiece);
+        } else {
+          const u32x2 x = *reinterpret_cast<const u32x2 *>(p + off + 8 * lpiece);
+          raw[i] = u32x4{x.x, x.y, 0, 0};
+        }
       }
-    }
-    // (lanes 0 to 15 the keys' scales, 16 to 31 the values')
-    if constexpr (BITS < 16)
-      if (lane < 32) sraw = (lane < 16 ? a.c.ks : a.c.vs)[rows + row_of(lane & 15)];
+      // (16 lanes each: 0 to 15 the keys' scales, 16 to 31 the values')
+      if constexpr (BITS < 16)
+        if (lane >> 4 == (VALUE ? 1 : 0)) scale = (VALUE ? a.c.vs : a.c.ks)[rows + row_of(lane & 15)];
+    };
+    if constexpr (INSIDE) go([](int r) -> uint32_t { return r; });
+    else go([&](int r) -> uint32_t { return (uint32_t)held(k16 + r) & in_page; });
   };
   // codes as 16-bit values in LDS: keys in Q's type, values in fp16
-  auto widen = [&](uint32_t stage) {
+  auto widen = [&](auto value, const u32x4 (&raw)[NR], uint16_t scale, uint32_t tile_at, uint32_t scales) __attribute__((always_inline)) {
     if constexpr (BITS < 16) {
+      constexpr bool VALUE = decltype(value)::value, TO = BF16 && !VALUE;
       constexpr int WORDS = PIECE / 4, PER = BITS == 8 ? 2 : 1;   // words of a piece, words of 8 codes
 #pragma unroll
-      for (int i = 0; i < 2 * NL; i++) {
-        const bool value = i >= NL;
-        const int r = 16 * w + i % NL * LR + lrow;
-        const u32x4 raw = value ? vraw[i % NL] : kraw[i % NL];
+      for (int i = 0; i < NL; i++) {
+        const int r = 16 * w + i * LR + lrow;
 #pragma unroll
         for (int e = 0; e < WORDS / PER; e++) {
           uint32_t w0, w1, y0, y1, y2, y3;
-          if constexpr (BITS == 8) { w0 = raw[2 * e]; w1 = raw[2 * e + 1]; }
-          else tq4_to_fp8(raw[e], w0, w1);
-          if (BF16 && !value) {
-            widen4<true>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
-            widen4<true>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
-          } else {
-            widen4<false>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
-            widen4<false>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
-          }
-          *reinterpret_cast<u32x4 *>(smem + stage + (value ? VOFF : 0) + r * LB + 16 * ((lpiece * (WORDS / PER) + e) ^ swizzle(r, value))) =
-              u32x4{y0, y1, y2, y3};
+          if constexpr (BITS == 8) { w0 = raw[i][2 * e]; w1 = raw[i][2 * e + 1]; }
+          else tq4_to_fp8(raw[i][e], w0, w1);
+          widen4<TO>(w0, BITS == 4 ? 512.0f : 1.0f, y0, y1);
+          widen4<TO>(w1, BITS == 4 ? 512.0f : 1.0f, y2, y3);
+          *reinterpret_cast<u32x4 *>(smem + tile_at + r * LB + 16 * ((lpiece * (WORDS / PER) + e) ^ swizzle(r, VALUE))) = u32x4{y0, y1, y2, y3};
         }
       }
       // The keys' scales; the values' as binades and their inverse.  (A value scale of zero, whose
       // codes are zero, counts as fp16's smallest, and so does NaN, whose row is marked.)
-      float *const to = reinterpret_cast<float *>(smem + stage + SOFF) + 16 * w + (lane & 15);
-      const float x = half_bits_to_float(sraw);
-      if (lane < 16) {
-        to[0] = x;
-      } else if (lane < 32) {
-        const float y = fmaxf(x, kLeastScale);
-        to[KT] = __builtin_amdgcn_logf(y);
-        to[2 * KT] = 1.0f / y;
+      float *const to = reinterpret_cast<float *>(smem + scales) + 16 * w + (lane & 15);
+      const float x = half_bits_to_float(scale);
+      if (lane >> 4 == (VALUE ? 1 : 0)) {
+        if constexpr (!VALUE) {
+          to[0] = x;
+        } else {
+          const float y = fmaxf(x, kLeastScale);
+          to[0] = __builtin_amdgcn_logf(y);
+          to[KT] = 1.0f / y;
+        }
       }
-      const uint64_t nan = __ballot(x != x);
-      if (lane == 0) reinterpret_cast<uint16_t *>(smem + stage + SOFF + 12 * KT)[w] = (uint16_t)(nan >> 16);
+      if constexpr (VALUE) {
+        const uint64_t nan = __ballot(x != x);
+        if (lane == 0) reinterpret_cast<uint16_t *>(smem + scales + 8 * KT)[w] = (uint16_t)(nan >> 16);
+      }
     }
   };
 
   // ---- addresses of the two kinds of LDS reads
-  const uint32_t kx = LC > 8 ? lane & 15 : lane & 7;
+  const uint32_t kx = swizzle(r32, false);
   const uint32_t krow = r32 * LB;
   const int tq = lane >> 4, ti = lane & 15;
   const int vr = 4 * (tq >> 1) + (ti >> 2);
-  const uint32_t vx = LC > 8 ? 2 * (vr & 7) : 2 * (vr & 3);
+  const uint32_t vx = swizzle(vr, true);
   const uint32_t vrow = vr * LB + (ti & 1) * 8, vc = 2 * (tq & 1) + ((ti & 3) >> 1);
 
-  v16f sc[NK];
-  u32x4 pt[NK][2];
+  // A tile is taken in halves of 32 keys, i = 0, 1.
   auto key_of = [&](int i, int v) -> int { return 32 * i + 8 * (v >> 2) + 4 * half + (v & 3); };
-  auto scores = [&](int k, uint32_t stage) {
+  auto scale4 = [&](uint32_t scales, int i, int g) -> v4f { return *reinterpret_cast<const v4f *>(smem + scales + 4 * key_of(i, 4 * g)); };
+  const uint32_t count = (uint32_t)max(seen.hi - max(seen.lo, 0), 0) & (seen.lo < seen.hi ? 0xffffffffu : 0u);
+  auto masked = [&](int k, int i, int v) -> bool { return (uint32_t)(k + key_of(i, v) - seen.lo) >= count; };
+  // products of Q and half a tile's keys, times the keys' scales
+  auto times_scales = [&](v16f &sc, uint32_t kscales, int i) __attribute__((always_inline)) {
+    if constexpr (BITS < 16) {
 #pragma unroll
-    for (int i = 0; i < NK; i++) {
-      sc[i] = v16f{0};
+      for (int g = 0; g < 4; g++) {
+        const v4f x = scale4(kscales, i, g);
 #pragma unroll
-      for (int e = 0; e < KS; e++) {
-        const u32x4 op = *reinterpret_cast<const u32x4 *>(smem + stage + 32 * i * LB + krow + 16 * ((2 * e + half) ^ kx));
-        sc[i] = mfma32<BF16>(op, q[e], sc[i]);
-      }
-      if constexpr (BITS < 16) {
-#pragma unroll
-        for (int g = 0; g < 4; g++) {
-          const v4f ks = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * key_of(i, 4 * g));
-#pragma unroll
-          for (int j = 0; j < 4; j++) sc[i][4 * g + j] *= ks[j];
-        }
+        for (int j = 0; j < 4; j++) sc[4 * g + j] *= x[j];
       }
     }
+  };
+  constexpr bool BINADES = EXT || BITS < 16;
+  // Scores of half a tile from its products: in binades (16-bit rows without cap and bias: before
+  // their factor), values' scales among them; the reference moved where it has to be.
+  // edge: some row does not see all keys.
+  auto refer = [&](v16f &sc, int k, int i, uint32_t vscales, auto edge) __attribute__((always_inline)) {
     if constexpr (EXT) {
       if (a.cap > 0.0f) {
 #pragma unroll
-        for (int i = 0; i < NK; i++)
-#pragma unroll
-          for (int v = 0; v < 16; v++) sc[i][v] = capped(sc[i][v], shape);
+        for (int v = 0; v < 16; v++) sc[v] = capped(sc[v], shape);
       } else {
 #pragma unroll
-        for (int i = 0; i < NK; i++)
-#pragma unroll
-          for (int v = 0; v < 16; v++) sc[i][v] *= c1;
+        for (int v = 0; v < 16; v++) sc[v] *= c1;
       }
       if (a.slopes != nullptr) {
         const float far = (float)(k + 4 * half - pos);
 #pragma unroll
-        for (int i = 0; i < NK; i++)
-#pragma unroll
-          for (int v = 0; v < 16; v++) sc[i][v] = fmaf(-slope, fabsf(far + (float)(32 * i + 8 * (v >> 2) + (v & 3))), sc[i][v]);
+        for (int v = 0; v < 16; v++) sc[v] = fmaf(-slope, fabsf(far + (float)(32 * i + 8 * (v >> 2) + (v & 3))), sc[v]);
       }
     }
-  };
-  const uint32_t count = (uint32_t)max(seen.hi - max(seen.lo, 0), 0) & (seen.lo < seen.hi ? 0xffffffffu : 0u);
-  auto masked = [&](int k, int i, int v) -> bool { return (uint32_t)(k + key_of(i, v) - seen.lo) >= count; };
-  // the weights of the tile, rounded, in pt; edge: some row does not see all of its keys
-  auto softmax = [&](int k, uint32_t stage, auto edge) {
     if constexpr (decltype(edge)::value) {
 #pragma unroll
-      for (int i = 0; i < NK; i++)
-#pragma unroll
-        for (int v = 0; v < 16; v++) sc[i][v] = masked(k, i, v) ? -INFINITY : sc[i][v];
+      for (int v = 0; v < 16; v++) sc[v] = masked(k, i, v) ? -INFINITY : sc[v];
     }
-    // scores in binades above no reference yet, values' scales among them: t = s + log2(scale)
-    float y = -INFINITY;
     if constexpr (BITS < 16) {
 #pragma unroll
-      for (int i = 0; i < NK; i++)
+      for (int g = 0; g < 4; g++) {
+        const v4f x = scale4(vscales, i, g);
 #pragma unroll
-        for (int g = 0; g < 4; g++) {
-          const v4f x = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * (KT + key_of(i, 4 * g)));
-#pragma unroll
-          for (int j = 0; j < 4; j++) sc[i][4 * g + j] = EXT ? sc[i][4 * g + j] + x[j] : fmaf(sc[i][4 * g + j], c1, x[j]);
-        }
+        for (int j = 0; j < 4; j++) sc[4 * g + j] = EXT ? sc[4 * g + j] + x[j] : fmaf(sc[4 * g + j], c1, x[j]);
+      }
     }
-    constexpr bool BINADES = EXT || BITS < 16;
+    float y = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < NK; i++)
-#pragma unroll
-      for (int v = 0; v < 16; v++) y = fmaxf(y, sc[i][v]);
+    for (int v = 0; v < 16; v++) y = fmaxf(y, sc[v]);
     if constexpr (!BINADES) y *= c1;
     if (__any(y - m > most)) {   // (also the first finite score)
       // (only that row's: what a row gives does not depend on the rows beside it)
@@ -403,61 +393,17 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
       m = m1;
       l *= f;
 #pragma unroll
-      for (int i = 0; i < DT; i++)
+      for (int c = 0; c < DT; c++)
 #pragma unroll
-        for (int v = 0; v < 16; v++) o[i][v] *= f;
+        for (int v = 0; v < 16; v++) o[c][v] *= f;
     }
-#pragma unroll
-    for (int i = 0; i < NK; i++)
-#pragma unroll
-      for (int v = 0; v < 16; v++) sc[i][v] = __builtin_amdgcn_exp2f(BINADES ? sc[i][v] - m : fmaf(sc[i][v], c1, -m));
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NK; i++)
-#pragma unroll
-      for (int g = 0; g < 4; g++) {
-        if constexpr (BITS < 16) {
-          const v4f x = *reinterpret_cast<const v4f *>(smem + stage + SOFF + 4 * (2 * KT + key_of(i, 4 * g)));
-#pragma unroll
-          for (int j = 0; j < 4; j++) sum = fmaf(sc[i][4 * g + j], x[j], sum);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; j++) sum += sc[i][4 * g + j];
-        }
-      }
-    l += sum;
   };
-  auto values_of = [&](uint32_t at_lds, int i, int t, int c) -> u32x4 {
-    const uint8_t *p = smem + at_lds + (32 * i + 16 * t) * LB + vrow + 16 * ((4 * c + vc) ^ vx);
+  // keys 16 t .. 16 t + 15 of half a tile, channels 32 c .. 32 c + 31
+  auto values_of = [&](uint32_t at_lds, int t, int c) -> u32x4 {
+    const uint8_t *p = smem + at_lds + 16 * t * LB + vrow + 16 * ((4 * c + vc) ^ vx);
     const u32x2 x = read_columns(p), y = read_columns(p + 8 * LB);
     return u32x4{x.x, x.y, y.x, y.y};
   };
-  // O^T += V^T P^T: the weights rounded, and (fine) what that leaves of them
-  auto products = [&](uint32_t at_lds) {
-#pragma unroll
-    for (int term = 0; term < (FINE ? 2 : 1); term++) {
-#pragma unroll
-      for (int i = 0; i < NK; i++)
-#pragma unroll
-        for (int t = 0; t < 2; t++)
-#pragma unroll
-          for (int j = 0; j < 4; j++) {
-            float x = sc[i][8 * t + 2 * j], y = sc[i][8 * t + 2 * j + 1];
-            if (term > 0) {
-              x -= lower_half<VBF>(pt[i][t][j]);
-              y -= upper_half<VBF>(pt[i][t][j]);
-            }
-            pt[i][t][j] = pack2<VBF>(x, y);
-          }
-#pragma unroll
-      for (int c = 0; c < DT; c++)
-#pragma unroll
-        for (int i = 0; i < NK; i++)
-#pragma unroll
-          for (int t = 0; t < 2; t++) o[c] = mfma32<VBF>(values_of(at_lds, i, t, c), pt[i][t], o[c]);
-    }
-  };
-
   // ---- the tiles: first those that all rows see whole, [p0, p1), then the others
   int p0 = k0, p1 = k0;
   if (all_lo_max < all_hi_min) {
@@ -468,100 +414,190 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D)) void prompt_ke
   // the t-th of all tiles in that order, t counted in keys (past the last one: any)
   auto tile_at = [&](int t) -> int { return t < skip ? p0 + t : t - skip < p0 - k0 ? k0 + t - skip : k0 + t; };
   const int end = k1 - k0;
-  uint32_t stage = 0;
+
+  // Keys are half a tile ahead: while half a tile's scores become weights and enter the products
+  // with the values, the products of Q and the next half's keys are formed, so that the matrix
+  // cores and the vector ALU both have work all the time.  A step's loads are therefore the
+  // values of the next tile, the second half of its keys (wavefronts 2, 3), and the first half
+  // of the keys of the tile behind it (0, 1): each into a place that the step before was the
+  // last to read.
+  typedef std::true_type Value;
+  typedef std::false_type Key;
+  const int lead = w < 2 ? 2 * KT : KT;
+  v16f sa = {0}, sb = {0};
+  int kpage = 0, vpage = 0;
   if (end > 0) {
-    load_page(tile_at(0));
-    load(tile_at(0), 0, std::false_type());
-    widen(0);
-    load_page(tile_at(KT));
+    vpage = page_of(tile_at(0));
+    kpage = page_of(tile_at(KT));
+    load(Key(), kraw, kscale, tile_at(0), vpage, key_tile(0), std::false_type());
+    load(Value(), vraw, vscale, tile_at(0), vpage, value_tile(0), std::false_type());
+    widen(Key(), kraw, kscale, key_tile(0), key_scales(0));
+    widen(Value(), vraw, vscale, value_tile(0), value_scales(0));
+    vpage = kpage;
+    if (KT < end && w < 2) {
+      load(Key(), kraw, kscale, tile_at(KT), kpage, key_tile(1), std::false_type());
+      widen(Key(), kraw, kscale, key_tile(1), key_scales(1));
+      kpage = page_of(tile_at(2 * KT));
+    }
+    wait_all();
+    if (live) {
+#pragma unroll
+      for (int e = 0; e < KS; e++)
+        sa = mfma32<BF16>(*reinterpret_cast<const u32x4 *>(smem + key_tile(0) + krow + 16 * ((2 * e + half) ^ kx)), q[e], sa);
+      times_scales(sa, key_scales(0), 0);
+    }
   }
   int t = 0;
-  // a tile's data is there, and the next one's on its way
-  auto next = [&]() {
+  // The data of step t is there; that of the next one on its way.  odd: t / 64 mod 2.  fast: two
+  // more tiles that all rows see whole follow.
+  auto next = [&](int odd, auto fast) __attribute__((always_inline)) {
     wait_all();
-    if (t + KT < skip) load(p0 + t + KT, STAGE - stage, std::true_type());
-    else if (t + KT < end) load(tile_at(t + KT), STAGE - stage, std::false_type());
-    load_page(tile_at(t + 2 * KT));
+    const uint32_t keys = w < 2 ? key_tile(odd) : key_tile(1 - odd);
+    if constexpr (decltype(fast)::value) {
+      load(Key(), kraw, kscale, p0 + t + lead, kpage, keys, std::true_type());
+      load(Value(), vraw, vscale, p0 + t + KT, vpage, value_tile(1 - odd), std::true_type());
+      kpage = page_of(p0 + t + KT + lead);
+      vpage = page_of(p0 + t + 2 * KT);
+    } else {
+      if (t + lead < end) load(Key(), kraw, kscale, tile_at(t + lead), kpage, keys, std::false_type());
+      if (t + KT < end) load(Value(), vraw, vscale, tile_at(t + KT), vpage, value_tile(1 - odd), std::false_type());
+      kpage = page_of(tile_at(t + KT + lead));
+      vpage = page_of(tile_at(t + 2 * KT));
+    }
     if constexpr (BITS < 16) {
       // rows whose value scale is NaN read as NaN
-      const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + stage + SOFF + 12 * KT);
+      const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + value_scales(odd) + 8 * KT);
       if (uniform((int)(nan | nan >> 32)) != 0) {
         for (int i = threadIdx.x; i < KT * LC; i += T)
-          if (nan >> (i / LC) & 1) *reinterpret_cast<u32x4 *>(smem + stage + VOFF + 16 * i) = u32x4{0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u};
+          if (nan >> (i / LC) & 1) *reinterpret_cast<u32x4 *>(smem + value_tile(odd) + 16 * i) = u32x4{0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u};
         wait_lds();
       }
     }
   };
-  auto done = [&]() {
-    if (t + KT < end) widen(STAGE - stage);
-    stage = STAGE - stage;
+  auto done = [&](int odd, auto fast) __attribute__((always_inline)) {
+    constexpr bool ON = decltype(fast)::value;
+    if (ON || t + lead < end) widen(Key(), kraw, kscale, w < 2 ? key_tile(odd) : key_tile(1 - odd), w < 2 ? key_scales(odd) : key_scales(1 - odd));
+    if (ON || t + KT < end) widen(Value(), vraw, vscale, value_tile(1 - odd), value_scales(1 - odd));
+    t += KT;
   };
-  for (; t < skip; t += KT) {
-    next();
-    if (live) {
-      scores(tile_at(t), stage);
-      softmax(tile_at(t), stage, std::false_type());
-      products(stage + VOFF);
+  // Half i of step t: one matrix product at a time with its share of the vector work behind it,
+  // in this order.  A product occupies the matrix core for 32 cycles, in which its wavefront
+  // issues five or six other instructions; operands are read some products before their use.
+  auto half_step = [&](v16f &now, v16f &then, int i, int odd, int k, auto edge) __attribute__((always_inline)) {
+    constexpr int NQ = KS, NV = 2 * DT, ALL = NQ + (FINE ? 2 : 1) * NV, AHEAD = BITS < 16 ? 4 : 8;
+    u32x4 ring[AHEAD], pt[2];
+    // (past the last tile: keys of what is there, for nothing)
+    const uint32_t keys = i == 0 ? key_tile(odd) + 32 * LB : key_tile(1 - odd), values = value_tile(odd) + 32 * i * LB;
+    auto operand = [&](int n) -> u32x4 {
+      if (n < NQ) return *reinterpret_cast<const u32x4 *>(smem + keys + krow + 16 * ((2 * n + half) ^ kx));
+      const int e = (n - NQ) % NV;
+      return values_of(values, e / DT, e % DT);
+    };
+#pragma unroll
+    for (int n = 0; n < AHEAD - 1; n++) ring[n] = operand(n);
+    __builtin_amdgcn_sched_barrier(0);
+    refer(now, k, i, value_scales(odd), edge);
+    float sum = 0.0f;
+    then = v16f{0};
+#pragma unroll
+    for (int n = 0; n < ALL; n++) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (n + AHEAD - 1 < ALL) ring[(n + AHEAD - 1) % AHEAD] = operand(n + AHEAD - 1);
+      const u32x4 op = ring[n % AHEAD];
+      if (n < NQ) {
+        then = mfma32<BF16>(op, q[n], then);
+#pragma unroll
+        for (int x = 16 * n / NQ; x < 16 * (n + 1) / NQ; x++) {
+          const float z = now[x], y = __builtin_amdgcn_exp2f(BINADES ? z - m : fmaf(z, c1, -m));
+          now[x] = y;
+          if (x & 1) pt[x / 8][x / 2 % 4] = pack2<VBF>(now[x - 1], y);
+        }
+      } else {
+        const int e = (n - NQ) % NV;
+        if (n == NQ + NV) {      // what the rounding left
+#pragma unroll
+          for (int x = 0; x < 16; x += 2) {
+            const uint32_t z = pt[x / 8][x / 2 % 4];
+            pt[x / 8][x / 2 % 4] = pack2<VBF>(now[x] - lower_half<VBF>(z), now[x + 1] - upper_half<VBF>(z));
+          }
+        }
+        o[e % DT] = mfma32<VBF>(op, pt[e / DT], o[e % DT]);
+        if (n < NQ + NV) {
+#pragma unroll
+          for (int x = 16 * e / NV; x < 16 * (e + 1) / NV; x++) {
+            if constexpr (BITS < 16) sum = fmaf(now[x], reinterpret_cast<const float *>(smem + value_scales(odd))[KT + key_of(i, x)], sum);
+            else sum += now[x];
+          }
+        }
+      }
     }
-    done();
+    __builtin_amdgcn_sched_barrier(0);
+    // (now: the step's end is free to overwrite these scales' place, as that of their keys)
+    times_scales(then, key_scales(i == 0 ? odd : 1 - odd), 1 - i);
+    l += sum;
+  };
+  auto step = [&](int odd, auto fast, auto edge, int k) __attribute__((always_inline)) {
+    if constexpr (!decltype(edge)::value) next(odd, fast);
+    if (live) {
+      half_step(sa, sb, 0, odd, k, edge);
+      half_step(sb, sa, 1, odd, k, edge);
+    }
+    done(odd, fast);
+  };
+  typedef std::true_type Yes;
+  typedef std::false_type No;
+  while (t + 4 * KT <= skip) {
+    step(0, Yes(), No(), p0 + t);
+    step(1, Yes(), No(), p0 + t);
   }
-  for (; t < end; t += KT) {
-    next();
-    const int k = tile_at(t);
-    const bool here = live && k < hi_max && k + KT > lo_min;
+  while (t < skip) step(t / KT & 1, No(), No(), p0 + t);
+  while (t < end) {
+    const int odd = t / KT & 1, k = tile_at(t);
+    next(odd, No());
     // is a value not finite?
+    auto value_at = [&](int i) -> u32x4 & { return *reinterpret_cast<u32x4 *>(smem + value_tile(odd) + 16 * (i * T + (int)threadIdx.x)); };
+    constexpr int NV = TB / (16 * T);
     uint32_t bad = 0;
 #pragma unroll
-    for (int i = 0; i < KT * LB / (16 * T); i++) {
-      const u32x4 x = *reinterpret_cast<const u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
+    for (int i = 0; i < NV; i++) {
+      const u32x4 x = value_at(i);
 #pragma unroll
       for (int j = 0; j < 4; j++) bad |= not_finite<VBF>(x[j]);
     }
     if (__any(bad != 0) && lane == 0) *flag = t + 1;
-    if (here) {
-      scores(k, stage);
-      softmax(k, stage, std::true_type());
-    }
     wait_lds();
     if (uniform(*flag) == t + 1) {
-      // the keys have been read: their place takes ones where a value is not finite
+      // ones where a value is not finite, times ones where a row sees it, leave NaN; then zeros there
+      auto mask_of = [&](uint32_t x) -> uint32_t { return (not_finite<VBF>(x) >> 15) * 0xffffu; };
+      for (int c = 0; c < DT; c++) {
+        // (32 channels at a time, read as ones from where the values lie)
+        v16f n = {0};
 #pragma unroll
-      for (int i = 0; i < KT * LB / (16 * T); i++) {
-        u32x4 *const v = reinterpret_cast<u32x4 *>(smem + stage + VOFF + 16 * (i * T + (int)threadIdx.x));
-        u32x4 x = *v, y;
+        for (int h = 0; h < 4; h++) {
+          u32x4 op = values_of(value_tile(odd) + 32 * (h / 2) * LB, h % 2, c), ones;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const uint32_t b = (not_finite<VBF>(x[j]) >> 15) * 0xffffu;
-          y[j] = b & (kOne << 16 | kOne);
-          x[j] &= ~b;
+          for (int j = 0; j < 4; j++) {
+            op[j] = mask_of(op[j]) & (kOne << 16 | kOne);
+            ones[j] = (masked(k, h / 2, 8 * (h % 2) + 2 * j) ? 0u : kOne) | (masked(k, h / 2, 8 * (h % 2) + 2 * j + 1) ? 0u : kOne << 16);
+          }
+          n = mfma32<VBF>(op, ones, n);
         }
-        *v = x;
-        *reinterpret_cast<u32x4 *>(smem + stage + 16 * (i * T + (int)threadIdx.x)) = y;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+          for (int v = 0; v < 16; v++) o[d][v] = d == c && n[v] > 0.0f ? NAN : o[d][v];
       }
       wait_lds();
-      if (here) {
-        u32x4 ones[NK][2];
 #pragma unroll
-        for (int i = 0; i < NK; i++)
+      for (int i = 0; i < NV; i++) {
+        u32x4 x = value_at(i);
 #pragma unroll
-          for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int j = 0; j < 4; j++)
-              ones[i][h][j] = (masked(k, i, 8 * h + 2 * j) ? 0u : kOne) | (masked(k, i, 8 * h + 2 * j + 1) ? 0u : kOne << 16);
-#pragma unroll
-        for (int c = 0; c < DT; c++) {
-          v16f n = {0};
-#pragma unroll
-          for (int i = 0; i < NK; i++)
-#pragma unroll
-            for (int h = 0; h < 2; h++) n = mfma32<VBF>(values_of(stage, i, h, c), ones[i][h], n);
-#pragma unroll
-          for (int v = 0; v < 16; v++) o[c][v] = n[v] > 0.0f ? NAN : o[c][v];
-        }
+        for (int j = 0; j < 4; j++) x[j] &= ~mask_of(x[j]);
+        value_at(i) = x;
       }
+      wait_lds();
     }
-    if (here) products(stage + VOFF);
-    done();
+    step(odd, No(), Yes(), k);
   }
 
   // ---- results
