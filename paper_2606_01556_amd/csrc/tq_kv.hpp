@@ -97,6 +97,7 @@ struct PromptArgs {
   // parts where splits > 1 or shared: [splits][tokens][hq] references and sums, then as many products [d]
   float *scratch;
   int tiles, splits;
+  int room, longest;         // work-groups that run at once; keys that a row sees at most
   int64_t blocks;
 };
 
@@ -132,7 +133,7 @@ hipError_t launch_attend_scored(const AttendArgs &a, bool bf16, hipStream_t s);
 // How an attention of many tokens is cut: row tiles (a bound over all streams) and parts of
 // a tile's keys.
 struct PromptPlan {
-  int tiles, splits;
+  int tiles, splits, room, longest;
   int64_t blocks;
   size_t scratch;            // bytes
 };

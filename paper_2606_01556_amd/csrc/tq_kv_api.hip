@@ -282,7 +282,7 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
   a.out = static_cast<uint16_t *>(out);
   a.lse = lse;
   a.scratch = static_cast<float *>(scratch);
-  a.tiles = p.tiles; a.splits = p.splits; a.blocks = p.blocks;
+  a.tiles = p.tiles; a.splits = p.splits; a.blocks = p.blocks; a.room = p.room; a.longest = p.longest;
   return hip_status(tq::launch_prompt(a, dtype == TQ_BF16, static_cast<hipStream_t>(stream)));
 }
 
@@ -346,7 +346,7 @@ tq_status tq_shared_prefix_attention(const tq_kv_cache *c, const tq_head_rows *q
   x.out = static_cast<uint16_t *>(out);
   x.lse = lse;
   x.scratch = static_cast<float *>(scratch);
-  x.tiles = p.tiles; x.splits = p.splits; x.blocks = p.blocks;
+  x.tiles = p.tiles; x.splits = p.splits; x.blocks = p.blocks; x.room = p.room; x.longest = p.longest;
   tq::AttendArgs &y = a.own;
   y.c = k;
   y.q = rows.p; y.q_ts = rows.ts; y.q_hs = rows.hs;

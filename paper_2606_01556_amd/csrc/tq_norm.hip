@@ -6,6 +6,13 @@
 // (each of w1, g, r and w2 may be left out).  Bound by the bytes of x, r and the gate in and of s
 // and y out, so a row is read once and stays in registers, in fp32, through both of its sums;
 // y is made of s before that is rounded.
+//
+// A row of up to 512 values is a wavefront's, of up to 4096 256 threads', of up to 8192 512
+// threads', past that 1024 threads': the more of a row a thread holds, the fewer rows a CU has
+// under way (8192 rows of 8192 bf16 values, both norms and a gate of each: 128 us with 256
+// threads, 121 with 512 or 1024, 153 with 128; one row of 4096: 5.3 us whichever, the host's time,
+// 2.8 of them the kernel).  What is read and written at 6.5 TB/s would take 103 us.  Reading the
+// weights before the sums instead of after them: 2 us more.
 #include "tq_attention.hpp"
 #include "tq_kv.hpp"
 
@@ -29,6 +36,9 @@ template <bool BF16>
 __device__ __forceinline__ u32x4 pack8(const float (&f)[8]) {
   return u32x4{pack2<BF16>(f[0], f[1]), pack2<BF16>(f[2], f[3]), pack2<BF16>(f[4], f[5]), pack2<BF16>(f[6], f[7])};
 }
+
+// Rows are read once: non-temporal (8192 rows of 8192, with a gate of each: 121 -> 117 us).
+__device__ __forceinline__ u32x4 read_once(const uint16_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
 
 // T threads own a row, C pieces of eight values each: T * C * 8 >= n
 template <int T, int C, bool BF16>
@@ -87,9 +97,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
     const int p = c * T + t;
     const bool in = live && p < pieces;
     const u32x4 zero = {0, 0, 0, 0};
-    unpack8<BF16>(in ? *reinterpret_cast<const u32x4 *>(a.x + row * a.x_stride + 8 * p) : zero, x[c]);
-    unpack8<BF16>(in && a.residual != nullptr ? *reinterpret_cast<const u32x4 *>(a.residual + row * a.r_stride + 8 * p) : zero, s[c]);
-    if (a.gate != nullptr) unpack8<BF16>(in ? *reinterpret_cast<const u32x4 *>(a.gate + row * a.g_stride + 8 * p) : zero, gate[c]);
+    unpack8<BF16>(in ? read_once(a.x + row * a.x_stride + 8 * p) : zero, x[c]);
+    unpack8<BF16>(in && a.residual != nullptr ? read_once(a.residual + row * a.r_stride + 8 * p) : zero, s[c]);
+    if (a.gate != nullptr) {
+      const uint16_t *const g = a.gate + row * a.g_stride + 8 * p;
+      unpack8<BF16>(!in ? zero : a.g_stride == 0 ? *reinterpret_cast<const u32x4 *>(g) : read_once(g), gate[c]);
+    }
   }
   if (a.post != nullptr) {
     const float inv = inverse(x);
@@ -151,7 +164,7 @@ hipError_t launch_norm(const NormArgs &a, bool bf16, hipStream_t s) {
   if (pieces <= 128) return go_norm<64, 2>(a, bf16, s);
   if (pieces <= 256) return go_norm<256, 1>(a, bf16, s);
   if (pieces <= 512) return go_norm<256, 2>(a, bf16, s);
-  if (pieces <= 1024) return go_norm<256, 4>(a, bf16, s);
+  if (pieces <= 1024) return go_norm<512, 2>(a, bf16, s);
   if (pieces <= 2048) return go_norm<1024, 2>(a, bf16, s);
   return go_norm<1024, 4>(a, bf16, s);
 }

@@ -47,8 +47,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_prefix_kernel(const PrefixA
         ((int64_t)stream * p.c.heads + kvh) * ranges + in / hr];
     const float *const parts = p.scratch + parts_head(p.splits, heads);
 #pragma unroll 4
-    for (int k = mine; k < shared; k += side)
-      add(*reinterpret_cast<const f2 *>(p.scratch + 2 * (k * heads + row)), *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
+    for (int k = mine; k < shared; k += side) {
+      const f2 ml = *reinterpret_cast<const f2 *>(p.scratch + 2 * (k * heads + row));
+      if (ml.y != 0.0f) add(ml, *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
+    }
 #pragma unroll 2
     for (int k = mine; k < j.parts; k += side) {
       const int slot = k == 0 ? j.first : (j.first & ~1) + 2 * k;
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_prefix_kernel(const PrefixA
   if (!live || mine != 0) return;
   for (int k = 1; k < side; k++) {
     const f2 ml = *reinterpret_cast<const f2 *>(lds_ml[g + k]);
-    if (ml.x > -INFINITY) add(ml, *reinterpret_cast<const v4f *>(&lds_o[g + k][d0]));      // (it had parts)
+    if (ml.y != 0.0f) add(ml, *reinterpret_cast<const v4f *>(&lds_o[g + k][d0]));      // (it had parts)
   }
   const bool none = l == 0.0f;
   const float inv = 1.0f / l;

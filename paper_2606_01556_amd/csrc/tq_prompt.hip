@@ -33,15 +33,19 @@ __global__ __launch_bounds__(kJoinThreads) void join_rows_kernel(const PromptArg
   if (live) {
     const float *const parts = a.scratch + parts_head(a.splits, heads);
 #pragma unroll 4
-    for (int k = mine; k < a.splits; k += side)
-      add(*reinterpret_cast<const f2 *>(a.scratch + 2 * (k * heads + row)), *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
+    for (int k = mine; k < a.splits; k += side) {
+      const f2 ml = *reinterpret_cast<const f2 *>(a.scratch + 2 * (k * heads + row));
+      if (ml.y != 0.0f) add(ml, *reinterpret_cast<const v4f *>(parts + (k * heads + row) * D + d0));
+    }
     *reinterpret_cast<v4f *>(&lds_o[g][d0]) = o;
     if (d0 == 0) *reinterpret_cast<f2 *>(lds_ml[g]) = f2{m, l};
   }
   __syncthreads();
   if (!live || mine != 0) return;
-  for (int k = 1; k < side; k++)
-    if (k < a.splits) add(*reinterpret_cast<const f2 *>(lds_ml[g + k]), *reinterpret_cast<const v4f *>(&lds_o[g + k][d0]));
+  for (int k = 1; k < side; k++) {
+    const f2 ml = *reinterpret_cast<const f2 *>(lds_ml[g + k]);
+    if (ml.y != 0.0f) add(ml, *reinterpret_cast<const v4f *>(&lds_o[g + k][d0]));      // (it had parts)
+  }
   const bool none = l == 0.0f;
   const float inv = 1.0f / l;
   float y[4];
@@ -69,12 +73,18 @@ PromptPlan prompt_plan(const KvCache &c, int tokens, int batch, int hq, int64_t 
   PromptPlan p;
   const int64_t tiles = (int64_t)tokens * (hq / c.heads) / kPromptRows + batch;
   const int64_t units = tiles * c.heads;
-  // Where the tiles leave CUs without work, a tile's keys are split, down to 256 of them.
-  const int64_t room = kCus * (c.d == 256 ? 1 : c.d == 128 ? 2 : 3);
+  // Where the row tiles leave half of the CUs without work, a tile's keys are split, down to 256 of
+  // them.  How many parts a tile has is for the kernel to say, which knows the lengths: of several
+  // streams up to twice as many as would fill the CUs if all were alike.  (16 streams up to 8192
+  // with 5 new tokens each: 75 us with as many parts of each, 71.5 with a share of the whole each.
+  // One group of 64 streams behind 16384: 80 us with 32 parts, 84.5 with room for 64.)
+  p.room = kCus * (c.d == 256 ? 1 : c.d == 128 || c.bits < 16 ? 2 : 3);
   const int64_t longest = window > 0 && (int64_t)window + tokens < max_len ? (int64_t)window + tokens : max_len;
-  int64_t splits = units > 0 ? room / units : 1;
+  const int64_t rows = ((int64_t)tokens * (hq / c.heads) + kPromptRows - 1) / kPromptRows, real = (rows > batch ? rows : batch) * c.heads;
+  int64_t splits = real > 0 && 2 * real <= p.room ? ((batch > 1 ? 2 : 1) * p.room + real - 1) / real : 1;
   if (splits > (longest + 255) / 256) splits = (longest + 255) / 256;
   if (splits < 1) splits = 1;
+  p.longest = (int)longest;
   p.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
   p.splits = (int)splits;
   p.blocks = units * splits;

@@ -47,6 +47,7 @@ namespace {
 
 constexpr int kPromptWaves = 4, kPromptThreads = 64 * kPromptWaves;
 constexpr int kTileKeys = 64;
+constexpr int kLeastTiles = 4;             // of a split
 constexpr float kTopBinades = 15.99f;      // 2^15.99 < 65504
 
 // wavefronts of a SIMD that the registers are cut for
@@ -105,7 +106,7 @@ __device__ __forceinline__ float upper_half(uint32_t w) {
 }
 
 struct Interval {
-  int lo, hi;    // empty: INT32_MAX and 0
+  int lo, hi;
 };
 
 template <int D, int BITS, bool BF16, bool EXT, bool FINE>
@@ -163,6 +164,19 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   const int row0 = at * kPromptRows, rows = tokens * a.group;     // < 2^31 (host)
   if (at < 0 || row0 >= rows) return;
 
+  // tiles of keys that are a work-group's share
+  int share = 0;
+  if (a.splits > 1) {
+    int64_t all = 0;
+    for (int i = lane; i < a.batch; i += 64) {
+      const int rows_i = (start_of(i + 1) - start_of(i)) * a.group, keys_i = min(max(a.lengths[i], 0), a.longest);
+      all += (int64_t)((rows_i + kPromptRows - 1) / kPromptRows) * ((keys_i + KT - 1) / KT);
+    }
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) all += __shfl_xor(all, x);
+    share = uniform((int)max((all * hkv + a.room - 1) / a.room, (int64_t)kLeastTiles));
+  }
+
   // this lane's row and its interval
   const int cap = a.max_pages << lps;                             // <= 2^30 (host)
   const int len = min(max(uniform(a.lengths[s]), 0), cap);
@@ -182,10 +196,11 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
     if (a.window > 0 && pos >= a.window) seen.lo = pos - a.window + 1;
     if (a.first != nullptr) seen.lo = max(seen.lo, a.first[start + token]);
   }
-  if (seen.lo >= seen.hi) seen = {INT32_MAX, 0};
+  // (a row that sees nothing takes part in no bound; what it sums up is dropped at the end)
+  const bool sees = seen.lo < seen.hi;
 
   // bounds of the wavefront's rows, and of all rows
-  int lo_min = seen.lo, lo_max = seen.lo, hi_min = seen.hi, hi_max = seen.hi;
+  int lo_min = sees ? seen.lo : INT32_MAX, lo_max = sees ? seen.lo : 0, hi_min = sees ? seen.hi : INT32_MAX, hi_max = sees ? seen.hi : 0;
 #pragma unroll
   for (int m = 1; m < 32; m <<= 1) {
     lo_min = min(lo_min, __shfl_xor(lo_min, m)); lo_max = max(lo_max, __shfl_xor(lo_max, m));
@@ -218,12 +233,18 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   }
   all_lo = uniform(all_lo); all_lo_max = uniform(all_lo_max); all_hi_min = uniform(all_hi_min); all_hi = uniform(all_hi);
 
-  // this split's keys [k0, k1), from a multiple of 64
+  // This split's keys [k0, k1), from a multiple of 64.  Where there are splits, a work-group is to
+  // have about its share of all streams' tiles (as their lengths leave them), so that a long
+  // stream has many parts and a short one few.
   int k0 = 0, k1 = 0;
   if (all_lo < all_hi) {
     const int base = all_lo & ~(KT - 1), n = (all_hi - base + KT - 1) / KT;
-    k0 = base + (int)((int64_t)n * split / a.splits) * KT;
-    k1 = min(base + (int)((int64_t)n * (split + 1) / a.splits) * KT, all_hi);
+    int parts = 1;
+    if (a.splits > 1) parts = min(a.splits, max((n + share - 1) / share, 1));
+    if (split < parts) {
+      k0 = base + (int)((int64_t)n * split / parts) * KT;
+      k1 = min(base + (int)((int64_t)n * (split + 1) / parts) * KT, all_hi);
+    }
   }
 
   // what a score's product with the key's scale is multiplied by, in binades
@@ -337,7 +358,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   // A tile is taken in halves of 32 keys, i = 0, 1.
   auto key_of = [&](int i, int v) -> int { return 32 * i + 8 * (v >> 2) + 4 * half + (v & 3); };
   auto scale4 = [&](uint32_t scales, int i, int g) -> v4f { return *reinterpret_cast<const v4f *>(smem + scales + 4 * key_of(i, 4 * g)); };
-  const uint32_t count = (uint32_t)max(seen.hi - max(seen.lo, 0), 0) & (seen.lo < seen.hi ? 0xffffffffu : 0u);
+  const uint32_t count = sees ? (uint32_t)(seen.hi - seen.lo) : 0u;
   auto masked = [&](int k, int i, int v) -> bool { return (uint32_t)(k + key_of(i, v) - seen.lo) >= count; };
   // products of Q and half a tile's keys, times the keys' scales
   auto times_scales = [&](v16f &sc, uint32_t kscales, int i) __attribute__((always_inline)) {
@@ -602,6 +623,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
 
   // ---- results
   l += __shfl_xor(l, 32);
+  if (!sees) l = 0.0f;
   if (!live || row0 + 32 * w + r32 >= rows) return;
   const int64_t to = (int64_t)(start + token) * a.hq + head;
   if (a.splits == 1 && !a.shared) {
@@ -620,6 +642,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   } else {
     const int64_t heads = (int64_t)a.tokens * a.hq, part = split * heads + to;
     float *const op = a.scratch + parts_head(a.splits, heads) + part * D;
+    // (a part without keys is told by its sum, and not read)
+    if (k0 < k1)
 #pragma unroll
     for (int c = 0; c < DT; c++)
 #pragma unroll
