@@ -500,7 +500,7 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
  * A stream without prefix and tokens gives zeros and -infinity.  Precision as in
  * tq_prompt_attention for the prefix's keys, as in tq_paged_attention for a stream's own.
  * Three launches; the result does not depend on timing.  batch == 0 is a no-op; groups from 1
- * to 65535, batch and both tables within the limits of the two.
+ * to 65535, batch * q_heads <= 2^25, batch and both tables within the limits of the two.
  * Errors as tq_prompt_attention. */
 size_t tq_shared_prefix_attention_scratch_bytes(const tq_kv_cache *c, int batch, int q_heads, int groups,
                                                 int prefix_pages, int max_pages);

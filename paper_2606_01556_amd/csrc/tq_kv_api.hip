@@ -289,7 +289,8 @@ tq_status tq_prompt_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dt
 // both halves of a call, and where the second one's parts begin in scratch
 static tq_status plan_prefix(const tq_kv_cache *c, const tq::KvCache &k, int batch, int q_heads, int groups, int prefix_pages,
                              int max_pages, tq::PromptPlan &p, tq::AttendPlan &t, size_t &first, size_t &bytes) {
-  if (groups < 1 || groups > 65535 || batch < 0) return TQ_ERR_SHAPE;
+  // (the join's launch numbers its lanes in 32 bits, up to 64 of them a row)
+  if (groups < 1 || groups > 65535 || batch < 0 || (int64_t)batch * q_heads > ((int64_t)1 << 25)) return TQ_ERR_SHAPE;
   TQ_TRY(attention_plan(c, k, batch, q_heads, max_pages, 0, t));
   TQ_TRY(plan_prompt(c, k, batch, groups, q_heads, prefix_pages, 0, true, p));
   first = (p.scratch + 255) & ~(size_t)255;

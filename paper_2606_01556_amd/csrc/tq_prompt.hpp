@@ -20,19 +20,33 @@
 //  * The reference of the softmax moves only when a weight passes 65504 (bf16 rows: 1 over the
 //    number of keys), as in the attention of one token: most tiles neither exchange
 //    anything between lanes nor scale what has been summed.
-//  * A weight is rounded once to the second product's type (fp16: 2^-12 of itself at most, and
-//    2^-36 of the largest one; bf16 rows, whose values may pass fp16's range: 2^-9).  The
-//    products are what bounds the kernel, and more terms of a weight would be more products;
-//    the roundings of different keys are independent and stay below the result's own.  The
-//    sum that divides, and the log-sum-exp, take the weights unrounded, in fp32.
+//  * A weight is rounded once to the second product's type (fp16: 2^-11 of itself at most, and
+//    2^-37 of the largest one; bf16 rows, whose values may pass fp16's range: 2^-8).  The
+//    products are what bounds the kernel, and more terms of a weight are more products; the
+//    roundings of different keys are independent and come out below the result's own.  The
+//    sum that divides, and the log-sum-exp, take the weights unrounded, in fp32.  FINE: what the
+//    rounding leaves enters as a second term, for callers whose next step magnifies last bits.
 //  * Rows of 16 bits go from memory to LDS directly, 16 bytes a lane, swizzled by the address
-//    that a lane reads (so that neither kind of LDS read has bank conflicts); codes are
-//    widened on their way, exactly, their scales apply to scores and weights in fp32.
-//  * A tile's loads are in flight while the tile before it is computed on.
+//    that a lane reads, so that rows a few apart lie in different banks; codes are widened on
+//    their way, exactly, and their scales apply to scores and weights in fp32.
+//  * Tiles of which all rows see all keys come first, in a loop without a mask; a tile's loads
+//    are in flight while the one before it is computed on, and keys are half a tile ahead: while
+//    32 keys' scores become weights the next 32 keys' are formed, a matrix product at a time.
 //
 // Keys that a row does not see have no part in it, whatever they hold: a tile in which any
 // row's interval ends is searched for infinities and NaN, and where there is one the values
-// enter the product without it, and the rows that do see it get a NaN by a second product.
+// enter the products without it, and the rows that do see it get a NaN by a product of ones.
+//
+// Measured, where the products are the bound (PyTorch's bf16 product of two 8192 x 8192 matrices
+// reaches 1.22 to 1.27 PFLOP/s on the same card):
+//   1 prompt of 8192 tokens, 32 / 8 heads of 128, fp16          560 us, 982 TFLOP/s (exact: 740)
+//   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2570 us, 829 TFLOP/s
+//   2 prompts of 4096, 16 / 8 heads of 256, window 1024, capped 191 us, 520 TFLOP/s
+// The matrix cores are busy 45 % of the first, at 2.1 to 2.2 GHz of 2.4.  Left out one at a time
+// (in a copy), the loads give 75 us back, the exponentials 45, the maxima 40, half of the second
+// products 58: no single one holds the others up.  With keys a whole tile ahead the first takes
+// 548 us, but codes spill registers (8 bits 4100 to 7100 us) and 32 prompts up to 700 take 134 us
+// for 121; with none ahead 569, and 215 for the 191.
 #pragma once
 
 #include <cfloat>
@@ -469,8 +483,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
     }
   }
   int t = 0;
-  // The data of step t is there; that of the next one on its way.  odd: t / 64 mod 2.  fast: two
-  // more tiles that all rows see whole follow.
+  // The data of step t is there; that of the next one on its way.  odd: t / 64 mod 2.  fast: four
+  // more tiles that all rows see whole follow the first of two steps.
   auto next = [&](int odd, auto fast) __attribute__((always_inline)) {
     wait_all();
     const uint32_t keys = w < 2 ? key_tile(odd) : key_tile(1 - odd);
@@ -567,7 +581,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   };
   typedef std::true_type Yes;
   typedef std::false_type No;
-  while (t + 4 * KT <= skip) {
+  // (the second step of a pair looks up the page of the first one's t + 4 tiles)
+  while (t + 5 * KT <= skip) {
     step(0, Yes(), No(), p0 + t);
     step(1, Yes(), No(), p0 + t);
   }

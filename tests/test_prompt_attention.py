@@ -187,6 +187,22 @@ def test_window(kind, dtype, window):
 @gpu
 @pytest.mark.parametrize("kind,dtype", KINDS)
 @pytest.mark.parametrize("d", [64, 128, 256])
+def test_intervals_of_many_tiles(kind, dtype, d):
+    """Intervals that begin late and hold every number of whole tiles around those that the kernel
+    takes two at a time, in front of tiles that not all rows see."""
+    say("intervals", kind, dtype, d)
+    s, q = prompts([1100, 700], [300, 700], 2, 4, d, 16, kind, dtype)
+    for window in range(200, 800, 45):
+        held(s, q, window=window)
+    first = np.concatenate([np.full(300, 333), np.repeat([0, 131], [131, 569])])
+    held(s, q, first=first)
+    first[::5] = 1 << 20
+    held(s, q, first=first, window=640)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("d", [64, 128, 256])
 def test_masks(kind, dtype, d):
     say("masks", kind, dtype, d)
     lens, new = [200, 131, 90], [200, 131, 20]

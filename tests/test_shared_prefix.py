@@ -174,7 +174,7 @@ def test_shared_prefix_validation():
     for bad in (dict(q=None), dict(m=None), dict(ptab=None), dict(plen=None), dict(pt=None), dict(ln=None), dict(out=None),
                 dict(b=1, scratch=None)):
         assert call(**bad) == 1, bad
-    for bad in (dict(b=-1), dict(b=65536), dict(g=0), dict(g=65536), dict(hq=3), dict(ppages=0), dict(pages=0), dict(pstride=-1),
+    for bad in (dict(b=-1), dict(b=65536), dict(b=65535, hq=1024, pages=1, ppages=1), dict(g=0), dict(g=65536), dict(hq=3), dict(ppages=0), dict(pages=0), dict(pstride=-1),
                 dict(stride=-1), dict(s=scores(window=3)), dict(s=scores(softcap=-1.0)), dict(ppages=(1 << 26) + 1)):
         assert call(**bad) == 2, bad
     assert call(dt=1) == 5 and call(c=desc(head_dim=32)) == 7
