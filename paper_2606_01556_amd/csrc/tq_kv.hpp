@@ -1,6 +1,6 @@
 // Arguments and launch interface of the kernels between a block's linear
-// layers: norm and rotation of queries and keys, the paged key-value cache, and
-// the attention of one new token over it (internal to libtq).
+// layers: norm and rotation of queries and keys, the paged key-value cache, the
+// attentions over it, and the norms between blocks (internal to libtq).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -149,34 +149,45 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   const int tile = a.tiles - 1 - unit / a.splits;
 
   auto start_of = [&](int i) -> int { return min(max(a.starts[i], 0), a.tokens); };
-  // Stream i's tiles are numbered from floor(rows before it / 128) + i: numbers enough for
-  // each, in order, without a sum over the streams.
-  auto first_tile = [&](int i) -> int { return (int)(((int64_t)start_of(i) * a.group) / kPromptRows) + i; };
 
-  // rows of no stream (in shared mode the join leaves them to the tokens' own keys)
-  if (!a.shared && threadIdx.x < 64) {
-    const int begin = start_of(0), end = start_of(a.batch), none = begin + a.tokens - end;
-    for (int i = blockIdx.x; i < none; i += gridDim.x) {
-      const int64_t row = (int64_t)(i < begin ? i : i - begin + end) * a.hq;
+  // rows of no stream, cleared at the end (in shared mode the join leaves them to the tokens' own keys)
+  const int stream_rows = a.shared ? 0 : start_of(0), stream_end = a.shared ? a.tokens : start_of(a.batch);
+  auto clear = [&]() {
+    if (threadIdx.x >= 64) return;
+    for (int i = blockIdx.x; i < stream_rows + a.tokens - stream_end; i += gridDim.x) {
+      const int64_t row = (int64_t)(i < stream_rows ? i : i - stream_rows + stream_end) * a.hq;
       for (int e = lane; e < a.hq * (D / 2); e += 64) reinterpret_cast<uint32_t *>(a.out + row * D)[e] = 0;
       if (a.lse != nullptr)
         for (int e = lane; e < a.hq; e += 64) a.lse[row + e] = -INFINITY;
     }
-  }
+  };
 
-  // the stream whose tile this is: the last with first_tile <= tile, 64 candidates at a time
-  int s = 0;
-  for (int n = a.batch; n > 1;) {
+  // The stream whose tile this is.  Stream i's tiles are numbered from floor(rows before it / 128) +
+  // i: numbers enough for each, in order, without a sum over the streams; so it is the last whose
+  // first number is not past this tile, found 64 candidates at a time, which bring its start, its
+  // end and its length along.
+  int s = 0, start, after, length;
+  for (int n = a.batch;;) {
     const int step = (n + 63) / 64, i = s + lane * step;
-    const bool before = lane * step < n && first_tile(i) <= tile;
+    const int first = start_of(min(i, a.batch)), long_ = a.lengths[min(i, a.batch - 1)];
+    const bool before = lane * step < n && (int)((int64_t)first * a.group / kPromptRows) + i <= tile;
     const int count = max(__builtin_popcountll(__ballot(before)), 1) - 1;
     s = uniform(s + count * step);
+    if (step == 1) {
+      start = uniform(__shfl(first, count));
+      length = uniform(__shfl(long_, count));
+      after = uniform(count < 63 ? __shfl(first, count + 1) : start_of(s + 1));
+      break;
+    }
     n = uniform(min(step, n - count * step));
   }
-  const int start = uniform(start_of(s)), tokens = uniform(start_of(s + 1)) - start;
-  const int at = tile - uniform(first_tile(s));
+  const int tokens = after - start;
+  const int at = tile - ((int)((int64_t)start * a.group / kPromptRows) + s);
   const int row0 = at * kPromptRows, rows = tokens * a.group;     // < 2^31 (host)
-  if (at < 0 || row0 >= rows) return;
+  if (at < 0 || row0 >= rows) {
+    clear();
+    return;
+  }
 
   // tiles of keys that are a work-group's share
   int share = 0;
@@ -193,7 +204,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
 
   // this lane's row and its interval
   const int cap = a.max_pages << lps;                             // <= 2^30 (host)
-  const int len = min(max(uniform(a.lengths[s]), 0), cap);
+  const int len = min(max(length, 0), cap);
   const bool live = row0 + 32 * w < rows;                         // the wavefront holds rows
   const int row = min(row0 + 32 * w + r32, rows - 1);
   const int token = (int)((uint32_t)row / (uint32_t)a.group), head = kvh * a.group + (row - token * a.group);
@@ -637,6 +648,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   }
 
   // ---- results
+  clear();
   l += __shfl_xor(l, 32);
   if (!sees) l = 0.0f;
   if (!live || row0 + 32 * w + r32 >= rows) return;

@@ -1,9 +1,10 @@
 """The operators between a decoder block's linear layers, for inference: norm and
 position rotation of queries and keys, the paged key-value cache in 16, 8 or 4
-bits, and the attention of one new token over it.
+bits, the attentions over it (of one new token, of many, behind a shared prefix),
+and the norms and the residual sum between blocks.
 
-Binding of the ``tq_kv_*``, ``tq_qk_*`` and ``tq_paged_attention`` entry points of
-``libtq.so``; the arithmetic runs in the library's HIP kernels.  As in the rest of
+Binding of the ``tq_kv_*``, ``tq_qk_*``, ``tq_*_attention*`` and ``tq_add_rms_norm``
+entry points of ``libtq.so``; the arithmetic runs in the library's HIP kernels.  As in the rest of
 the package, every tensor is checked before the call (the library sees pointers; the
 checks are native, in ``csrc/tq_torch.cpp``, since an eager decode step waits for its
 host work), nothing is synchronized, and ``stream`` (a torch stream or a hipStream_t;
@@ -15,6 +16,8 @@ A decode step of one block:
     ...
     q = tq.qk_norm_rope_append(cache, q, k, v, positions, table, slots, q_weight, k_weight)
     y = tq.paged_attention(cache, q, page_table, lengths)
+    ...
+    x, h = tq.add_rms_norm(o_projection_of_y, x, mlp_norm_weight)
 """
 from __future__ import annotations
 

@@ -476,3 +476,64 @@ def test_other_stream_and_graph(lens, new):
         torch.cuda.synchronize()
         for g, out in graphs:
             assert torch.equal(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS[:3])
+@pytest.mark.parametrize("lens,new", [([5000], [3]), ([40, 90], [40, 33])])
+def test_rows_of_no_stream(kind, dtype, lens, new):
+    """Rows before and behind the streams, whole and with split keys."""
+    say("no stream", kind, dtype, lens)
+    s, q = prompts(lens, new, 2, 4, 64, 16, kind, dtype, pad=150)
+    rows = sum(new)
+    ref, lse = s.call(q, return_lse=True)
+    assert (ref[rows:] == 0).all() and torch.isinf(lse[rows:]).all()
+    s.starts = s.starts + 70
+    got, got_lse = s.call(torch.cat((q[-70:], q[:-70])), return_lse=True)
+    assert torch.equal(got[70:70 + rows], ref[:rows]) and torch.equal(got_lse[70:70 + rows], lse[:rows])
+    rest = torch.cat((got[:70], got[70 + rows:]))
+    assert (rest == 0).all() and (torch.cat((got_lse[:70], got_lse[70 + rows:])) == -math.inf).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("page", [512, 32768])
+def test_large_pages(kind, dtype, page):
+    say("pages", kind, dtype, page)
+    s, q = prompts([700, 1, 600], [700, 1, 30], 1, 4, 64, page, kind, dtype)
+    held(s, q)
+    held(s, q, window=330)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_a_row_does_not_depend_on_its_neighbours(kind, dtype):
+    """The same rows beside others, and in another place of the call."""
+    say("neighbours", kind, dtype)
+    s, q = prompts([500, 420], [500, 420], 2, 4, 128, 16, kind, dtype)
+    ref = s.call(q)
+    other = q.clone()
+    other[::3] *= 9.0
+    got = s.call(other)
+    keep = torch.arange(920) % 3 != 0
+    assert torch.equal(got[keep], ref[keep])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["f16", "4"])
+def test_offsets_past_32_bits(kind):
+    """Pages past 4 GiB of the cache's tensors."""
+    say("offsets", kind)
+    heads, d, page = 8, 256, 64
+    pages = (1 << 32) // (heads * page * d * (2 if kind == "f16" else 0.5)) + 40
+    cache = tq.empty_kv_cache(int(pages), page, heads, d, 16 if kind == "f16" else 4)
+    s = Prompts([300, 80], [300, 5], heads, d, page, "f16" if kind == "f16" else "4", F16)
+    for big, small in zip(cache._t, s.cache._t):
+        if big is not None:
+            big[-s.cache.pages:] = small
+    q = randn(305, heads * 2, d, seed=9).half().cuda()
+    table, lengths = s.args()
+    starts = torch.from_numpy(s.starts).cuda()
+    ref = tq.prompt_attention(s.cache, q, starts, table, lengths)
+    got = tq.prompt_attention(cache, q, starts, torch.where(table < 0, table, table + (cache.pages - s.cache.pages)), lengths)
+    assert torch.equal(got, ref)
