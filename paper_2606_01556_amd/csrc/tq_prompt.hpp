@@ -42,11 +42,12 @@
 //   1 prompt of 8192 tokens, 32 / 8 heads of 128, fp16          560 us, 982 TFLOP/s (exact: 740)
 //   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2570 us, 829 TFLOP/s
 //   2 prompts of 4096, 16 / 8 heads of 256, window 1024, capped 191 us, 520 TFLOP/s
-// The matrix cores are busy 45 % of the first, at 2.1 to 2.2 GHz of 2.4.  Left out one at a time
-// (in a copy), the loads give 75 us back, the exponentials 45, the maxima 40, half of the second
-// products 58: no single one holds the others up.  With keys a whole tile ahead the first takes
-// 548 us, but codes spill registers (8 bits 4100 to 7100 us) and 32 prompts up to 700 take 134 us
-// for 121; with none ahead 569, and 215 for the 191.
+// The matrix cores are busy half of the first's cycles, without bank conflicts, and the clock is
+// at 1.9 GHz of 2.4: as steps took cycles away (1.38 million at first, 1.07 now) it went down
+// from 2.05.  Left out one at a time (in a copy), the loads give 75 us back, the exponentials 45,
+// the maxima 40, half of the second products 58: no single one holds the others up.  With keys a
+// whole tile ahead the first takes 548 us, but codes spill registers (8 bits 4100 to 7100 us) and
+// 32 prompts up to 700 take 134 us for 121; with none ahead 569, and 215 for the 191.
 #pragma once
 
 #include <cfloat>
