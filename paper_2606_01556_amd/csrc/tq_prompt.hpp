@@ -40,7 +40,7 @@
 // Measured, where the products are the bound (PyTorch's bf16 product of two 8192 x 8192 matrices
 // reaches 1.22 to 1.27 PFLOP/s on the same card):
 //   1 prompt of 8192 tokens, 32 / 8 heads of 128, fp16          560 us, 982 TFLOP/s (exact: 740)
-//   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2570 us, 829 TFLOP/s
+//   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2530 us, 842 TFLOP/s
 //   2 prompts of 4096, 16 / 8 heads of 256, window 1024, capped 191 us, 520 TFLOP/s
 // The matrix cores are busy half of the first's cycles, without bank conflicts, and the clock is
 // at 1.9 GHz of 2.4: as steps took cycles away (1.38 million at first, 1.07 now) it went down
@@ -546,6 +546,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
     refer(now, k, i, value_scales(odd), edge);
     float sum = 0.0f;
     then = v16f{0};
+    // (products go first: 8 bits 2595 -> 2530 us, 16 bits 1 % or less)
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int n = 0; n < ALL; n++) {
       __builtin_amdgcn_sched_barrier(0);
@@ -578,6 +580,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
         }
       }
     }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     // (now: the step's end is free to overwrite these scales' place, as that of their keys)
     times_scales(then, key_scales(i == 0 ? odd : 1 - odd), 1 - i);
