@@ -83,18 +83,6 @@ __device__ __forceinline__ void lwait_vm() {
   __builtin_amdgcn_s_waitcnt((N & 0xf) | ((N >> 4) << 14) | (0x7 << 4) | (0xf << 8));
 }
 
-// 16 bytes per lane from addr into LDS at lds + 16 * lane
-__device__ __forceinline__ void ldma(const uint8_t *addr, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds)
-               : "memory");
-}
-
-// the same with a wave-uniform base and a 32-bit lane offset
-__device__ __forceinline__ void ldma_s(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
-               : "memory");
-}
-
 // a wave-uniform pointer, kept in scalar registers
 __device__ __forceinline__ const uint8_t *l_uniform(const uint8_t *p) {
   const uint64_t v = reinterpret_cast<uint64_t>(p);
@@ -240,15 +228,15 @@ __global__ __launch_bounds__(64 * LW, 1) void dual_gemm_large_kernel(GemmArgs a,
         const int ct = min(n0 / 32 + wave, ct32 - 1);
 #pragma unroll
         for (int rb = 0; rb < C::RB; rb++)
-          ldma(a.packed + geo.off_l2 + (((int64_t)ct * C::RB + rb) * 64 + lane) * 16,
-               lds0 + C::OFF_L2 + (wave * C::RB + rb) * 1024);
+          load_to_lds(a.packed + geo.off_l2 + (((int64_t)ct * C::RB + rb) * 64 + lane) * 16,
+                      lds0 + C::OFF_L2 + (wave * C::RB + rb) * 1024);
       } else if (wave == 8) {
         const int q = lane < 8 * C::RB * 4 ? lane : 0;   // 4 pieces per (rank group, tile)
         const int h = q / 32, j = (q / 4) % 8, part = q % 4;
         const int col = min(n0 + 32 * j + 8 * part, geo.n_pad - 8);
         const int hg = h * 64 / geo.gr;   // rank group of 64-rank block h (gr >= 64 here)
-        ldma(a.packed + geo.off_l2s + ((int64_t)hg * geo.n_pad + col) * 2,
-             lds0 + C::OFF_L2 + 8 * C::RB * 1024);
+        load_to_lds(a.packed + geo.off_l2s + ((int64_t)hg * geo.n_pad + col) * 2,
+                    lds0 + C::OFF_L2 + 8 * C::RB * 1024);
       }
     }
   };
@@ -272,10 +260,10 @@ __global__ __launch_bounds__(64 * LW, 1) void dual_gemm_large_kernel(GemmArgs a,
     constexpr bool HW = decltype(HC)::value;   // this wavefront forms an H tile
     auto issue = [&](int g) {
       const uint32_t slot = lds0 + (g % D) * C::SLOT;
-      ldma_s(it0.off + (uint32_t)(GK == 1 ? g : g >> it0.shift) * it0.stride, l_uniform(it0.base), slot + it0.dst);
+      load_to_lds(it0.off + (uint32_t)(GK == 1 ? g : g >> it0.shift) * it0.stride, l_uniform(it0.base), slot + it0.dst);
       if constexpr (PER == 2) {
         const LItem it1 = l_item<RT>(a, wave + LW, lane, m0, n0);
-        ldma_s(it1.off + (uint32_t)(GK == 1 ? g : g >> it1.shift) * it1.stride, l_uniform(it1.base), slot + it1.dst);
+        load_to_lds(it1.off + (uint32_t)(GK == 1 ? g : g >> it1.shift) * it1.stride, l_uniform(it1.base), slot + it1.dst);
       }
     };
     auto group = [&](int g) {

@@ -125,18 +125,6 @@ __device__ __forceinline__ void wait_vm() {
 }
 __device__ __forceinline__ void wait_lgkm0() { __builtin_amdgcn_s_waitcnt(0xc07f); }
 
-// direct global -> LDS load of 16 bytes per lane into lds + 16 * lane:
-// scalar base + 32-bit lane offset
-__device__ __forceinline__ void dma_s(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase),
-               "s"(lds)
-               : "memory");
-}
-__device__ __forceinline__ void dma_v(const uint8_t *addr, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds)
-               : "memory");
-}
-
 // wave-uniform 64-bit pointer, kept in scalar registers
 __device__ __forceinline__ const uint8_t *uniform_ptr(const uint8_t *p) {
   const uint64_t v = reinterpret_cast<uint64_t>(p);
@@ -162,9 +150,9 @@ template <int GK>
 __device__ __forceinline__ void p_issue(const PPlan &P, bool three, int g, uint32_t slot_lds) {
   // the bases are wave-uniform (scalar registers): the block offset is added
   // with scalar instructions
-  dma_s(P.v1, P.b1 + (uint32_t)g * P.inc1, slot_lds + P.l1);
-  dma_s(P.v2, P.b2 + (uint32_t)g * P.inc2, slot_lds + P.l2);
-  if (three) dma_v(P.s3 + (uint64_t)(g / GK) * P.inc3, slot_lds + P_SW);
+  load_to_lds(P.v1, P.b1 + (uint32_t)g * P.inc1, slot_lds + P.l1);
+  load_to_lds(P.v2, P.b2 + (uint32_t)g * P.inc2, slot_lds + P.l2);
+  if (three) load_to_lds(P.s3 + (uint64_t)(g / GK) * P.inc3, slot_lds + P_SW);
 }
 
 // activation tile t of the block (clamped to the last tile): its group-0
@@ -221,7 +209,7 @@ struct HPlan {
 __device__ __forceinline__ void h_issue(const HPlan &P, int g, uint32_t slot_lds) {
 #pragma unroll
   for (int t = 0; t < 2; t++)
-    dma_v(P.base[t] + (uint64_t)(g >> P.shift[t]) * P.stride[t], slot_lds + P.lds[t]);
+    load_to_lds(P.base[t] + (uint64_t)(g >> P.shift[t]) * P.stride[t], slot_lds + P.lds[t]);
 }
 
 // items, in order: the 8 activation halves, RT L1 tiles, one scale item, then
@@ -734,17 +722,17 @@ __global__ __launch_bounds__(64 * PNW, 1) void dual_gemm_prefill_kernel(GemmArgs
         const int ct = min(n0 / 32 + 2 * wc + j, ctiles - 1);
 #pragma unroll
         for (int rbk = 0; rbk < C::RB; rbk++)
-          dma_s(lane * 16, uniform_ptr(l2codes + ((int64_t)ct * C::RB + rbk) * 1024),
-                l2_lds + (j * C::RB + rbk) * 1024);
+          load_to_lds(lane * 16, uniform_ptr(l2codes + ((int64_t)ct * C::RB + rbk) * 1024),
+                      l2_lds + (j * C::RB + rbk) * 1024);
       }
       // lane q < 8 RG: 8 scales of column tile j = q / (4 RG), rank group
       // (q / 4) % RG, columns 8 (q % 4) .. + 8
       const int q = lane & (8 * RG - 1);
       const int jj = q / (4 * RG), hg = (q / 4) % RG;
       const int ct = min(n0 / 32 + 2 * wc + jj, ctiles - 1);
-      dma_v(reinterpret_cast<const uint8_t *>(l2scales + (int64_t)hg * geo.n_pad + ct * 32 +
-                                              8 * (q & 3)),
-            l2_lds + 2 * C::RB * 1024);
+      load_to_lds(reinterpret_cast<const uint8_t *>(l2scales + (int64_t)hg * geo.n_pad + ct * 32 +
+                                                    8 * (q & 3)),
+                  l2_lds + 2 * C::RB * 1024);
     }
     if (wave == 0) K::template main_loop_pp<true, true, GK>(P, smem, ring_lds, KG, lane, wr, wc, acc);
     else if (wr == 0) K::template main_loop_pp<true, false, GK>(P, smem, ring_lds, KG, lane, wr, wc, acc);

@@ -83,10 +83,6 @@ __device__ __forceinline__ v16f mfma32(u32x4 a, u32x4 b, v16f c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
 
-// 16 bytes per lane from sbase + voff into LDS at lds + 16 * lane
-__device__ __forceinline__ void load_to_lds(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds) : "memory");
-}
 // a wave-uniform pointer, in scalar registers
 __device__ __forceinline__ const uint8_t *uniform_at(const uint8_t *p) {
   const uint64_t v = reinterpret_cast<uint64_t>(p);
