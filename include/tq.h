@@ -311,7 +311,7 @@ tq_status tq_act_codes_canonical(const void *x_codes, const void *x_scales, int 
  *               bits  8  head_dim e4m3 codes (OCP fp8, no infinities)
  *               bits  4  head_dim / 8 TQ4 code words
  *   k_scales, v_scales  [pages, kv_heads, page_size] fp16, one scale per row (8 and
- *             4 bits; NULL for 16).  A row stands for code * scale.
+ *             4 bits; NULL for 16), not negative.  A row stands for code * scale.
  * The quantizer is that of Sec. 2 Eq. (1) with the row as its group: scale =
  * fp16(max|x| / 7) and code = clamp(rint(x / scale), -7, 7) at 4 bits, fp16(max|x|
  * / 448) and x / scale rounded half to even to e4m3 at 8; a row whose scale is
@@ -464,9 +464,9 @@ tq_status tq_paged_attention_scored(const tq_kv_cache *c, const tq_head_rows *q,
  *   lse         [tokens, q_heads] fp32 or NULL
  *   scratch     device buffer of tq_prompt_attention_scratch_bytes bytes, 16-byte aligned, free
  *               again when the stream has run the call; may be NULL where that size is 0
- * What a row does not see (NaN too) has no effect on it; a value that is not finite leaves its
- * channel NaN or infinite in the rows that see it (8 and 4 bits: a scale that is NaN, all
- * channels).  Scores, softmax and sums are fp32; a weight enters the product with v rounded
+ * What a row does not see (NaN and infinities too, of scales as well) has no effect on it; a value
+ * that is not finite leaves its channel NaN or infinite in the rows that see it (8 and 4 bits: a
+ * value's scale that is not finite, all channels; the log-sum-exp stays the keys').  Scores, softmax and sums are fp32; a weight enters the product with v rounded
  * once, to 11 bits (16-bit cache of bf16 values: 8), unless exact; the divisor and the log-sum-exp take it
  * unrounded.  One launch, or two where the keys of a row are split; the result does not depend
  * on timing.  tokens == 0 is a no-op; batch from 1 to 65535 (0 with tokens == 0), max_pages *

@@ -69,7 +69,7 @@ constexpr float kTopBinades = 15.99f;      // 2^15.99 < 65504
 constexpr int prompt_occupancy(int d, int bits) { return d == 256 ? 1 : d == 128 || bits < 16 ? 2 : 3; }
 
 // Bytes of LDS: two tiles of keys, two of values, and (codes) what goes with them: the keys'
-// scales; the values' as binades and inverse, and which of them are NaN.  Then four bounds a
+// scales; the values' as binades and inverse, and which of them are not finite.  Then four bounds a
 // wavefront and a flag.
 constexpr int kKeyScales = kTileKeys * 4, kValueScales = kTileKeys * 8 + 16;
 constexpr int prompt_tiles(int d, int bits) { return kTileKeys * d * 8 + (bits < 16 ? 2 * (kKeyScales + kValueScales) : 0); }
@@ -350,20 +350,22 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
         }
       }
       // The keys' scales; the values' as binades and their inverse.  (A value scale of zero, whose
-      // codes are zero, counts as fp16's smallest, and so does NaN, whose row is marked.)
+      // codes are zero, counts as fp16's smallest, and so do infinity and NaN, whose rows are
+      // marked: binades of infinity would be added to the scores of rows that do not see it, too.)
       float *const to = reinterpret_cast<float *>(smem + scales) + 16 * w + (lane & 15);
       const float x = half_bits_to_float(scale);
+      const bool none = VALUE && (scale & 0x7c00u) == 0x7c00u;
       if (lane >> 4 == (VALUE ? 1 : 0)) {
         if constexpr (!VALUE) {
           to[0] = x;
         } else {
-          const float y = fmaxf(x, kLeastScale);
+          const float y = none ? kLeastScale : fmaxf(x, kLeastScale);
           to[0] = __builtin_amdgcn_logf(y);
           to[KT] = 1.0f / y;
         }
       }
       if constexpr (VALUE) {
-        const uint64_t nan = __ballot(x != x);
+        const uint64_t nan = __ballot(none);
         if (lane == 0) reinterpret_cast<uint16_t *>(smem + scales + 8 * KT)[w] = (uint16_t)(nan >> 16);
       }
     }
@@ -508,7 +510,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
       vpage = page_of(tile_at(t + 2 * KT));
     }
     if constexpr (BITS < 16) {
-      // rows whose value scale is NaN read as NaN
+      // rows whose value scale is not finite read as NaN
       const uint64_t nan = *reinterpret_cast<const uint64_t *>(smem + value_scales(odd) + 8 * KT);
       if (uniform((int)(nan | nan >> 32)) != 0) {
         for (int i = threadIdx.x; i < KT * LC; i += T)

@@ -537,3 +537,35 @@ def test_offsets_past_32_bits(kind):
     ref = tq.prompt_attention(s.cache, q, starts, table, lengths)
     got = tq.prompt_attention(cache, q, starts, torch.where(table < 0, table, table + (cache.pages - s.cache.pages)), lengths)
     assert torch.equal(got, ref)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS[2:])
+@pytest.mark.parametrize("lens,new", [([300, 77], [300, 50]), ([1500], [40])])
+def test_scales_that_are_not_finite(kind, dtype, lens, new):
+    """Infinite and NaN scales of rows that are not seen (behind a row, in another document, before a
+    window) have no part; an infinite scale of a value that is seen leaves no channel finite, and
+    the log-sum-exp the keys'."""
+    say("scales", kind, dtype, lens)
+    s, q = prompts(lens, new, 2, 4, 128, 16, kind, dtype)
+    n, t = lens[0], new[0]
+    row, page = t // 2, s.cache.page_size               # of stream 0; its key is not seen by those before it
+    slot = int(s.slots[0][n - t + row])
+    places = [(slot // page, slot % page)]
+    rows = np.arange(t)
+    for kw, hidden in ((dict(), rows < row), (dict(window=9), (rows < row) | (rows >= row + 9)),
+                       (dict(first=np.concatenate((np.where(rows > row, n - t + row + 1, 0), np.zeros(sum(new) - t)))), rows != row)):
+        hidden = torch.from_numpy(np.concatenate((hidden, np.ones(sum(new) - t, bool))))
+        ref, lse = s.call(q, return_lse=True, **kw)
+        for scales, values in ((s.cache.k_scales, False), (s.cache.v_scales, True)):
+            keep = scales.clone()
+            for value in (math.inf, -math.inf, math.nan):
+                for p, at in places:
+                    scales[p, :, at] = value
+                got, got_lse = s.call(q, return_lse=True, **kw)
+                assert torch.equal(got[hidden], ref[hidden]) and torch.equal(got_lse[hidden], lse[hidden]), (value, values)
+                if values:
+                    assert not torch.isfinite(got[~hidden].float()).any()
+                    # (the same sum from another reference, as in test_values_that_are_no_number)
+                    assert bool(((got_lse - lse).abs() <= 2.0 ** -16 * (1 + lse.abs())).all())
+                scales.copy_(keep)
