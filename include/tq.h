@@ -407,7 +407,7 @@ tq_status tq_kv_read(const tq_kv_cache *c, const int64_t *slots, int tokens, voi
  *               where that size is 0 (short streams)
  * What slots outside a stream's range hold (NaN too) has no effect.  A value of its
  * range that is not finite leaves its channel (8 and 4 bits: its row's channels) without a
- * finite number; an infinity may come out as NaN, since weights enter the products in
+ * finite number, and the log-sum-exp the keys'; an infinity may come out as NaN, since weights enter the products in
  * parts, of which some are zero.  Scores, the softmax and the sums are fp32; the softmax's weights enter the products with v with
  * all their bits (16-bit cache of bf16 values) or with 22, or to 2^-37 of the largest
  * weight (else).  One launch for short streams, else two; the result does not

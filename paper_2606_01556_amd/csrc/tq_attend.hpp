@@ -495,8 +495,11 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
-          for (int j = 0; j < 4; j++)
-            y = fmaxf(y, s[i][j] * c1 + (BITS < 16 ? fmaxf(__builtin_amdgcn_logf(scale_of(vs[i], j)), -24.0f) : 0.0f));
+          for (int j = 0; j < 4; j++) {
+            // (infinite scales, too, count as fp16's smallest here: p and its sum stay the keys')
+            const float binades = BITS < 16 ? __builtin_amdgcn_logf(scale_of(vs[i], j)) : 0.0f;
+            y = fmaxf(y, s[i][j] * c1 + (binades < 17.0f ? binades : -24.0f));
+          }
         y = fmaxf(y, __shfl_xor(y, 16));
         y = fmaxf(y, __shfl_xor(y, 32));
         const float m1 = fmaxf(m, y - headroom);

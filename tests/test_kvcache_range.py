@@ -66,6 +66,31 @@ def test_sum_with_values_that_are_no_number(kind, dtype, d):
     assert np.isnan(got[:6]).all() and (np.abs(got[6] - ref[6]) <= bound[6]).all()
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("kind,dtype", KINDS[2:])
+def test_sum_with_infinite_scales(kind, dtype, d):
+    """So do value rows whose scale is infinite (which the quantizer does not write): their streams have
+    no finite channel, the log-sum-exp is the keys', scored or not, alone or behind a shared prefix."""
+    lens = [1, 40, 3000, 60, 700, 33]
+    s = Held(lens, 2, d, 16, kind, dtype, seed=d)
+    q = randn(len(lens), 6, d, seed=3).to(dtype)
+    at = [int(s.slots[i][n // 2]) for i, n in enumerate(lens[:5])]
+    s.cache.v_scales[[x // 16 for x in at], :, [x % 16 for x in at]] = math.inf
+    s.cache.v_scales[[int(x) // 16 for x in s.slots[3]], :, [int(x) % 16 for x in s.slots[3]]] = math.inf      # (all rows)
+    got, lse = run(s, q)
+    ref, ref_lse, bound, lse_bound = s.plain(q, d ** -0.5, 0)
+    assert (np.abs(lse - ref_lse) <= lse_bound).all()
+    assert not np.isfinite(got[:5]).any() and (np.abs(got[5] - ref[5]) <= bound[5]).all()
+    # (slopes of zero, and a prefix of no tokens: as without)
+    table, lengths = s.args()
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for out, sums in (run(s, q, slopes=torch.zeros(6, device="cuda")), tq.shared_prefix_attention(
+            s.cache, q.cuda(), torch.tensor([0, len(lens)], dtype=torch.int32, device="cuda"), table[:1], none, table, lengths, return_lse=True)):
+        out, sums = (x.cpu().double().numpy() if hasattr(x, "cpu") else x for x in (out, sums))
+        assert (np.abs(sums - ref_lse) <= lse_bound).all()
+        assert not np.isfinite(out[:5]).any() and (np.abs(out[5] - ref[5]) <= bound[5]).all()
+
+
 @pytest.mark.parametrize("d,lens", [(64, [1, 40, 0, 5000]), (128, [300, 17, 9000]), (256, [200, 3]), (256, [4100, 64]), (64, [70000])])
 @pytest.mark.parametrize("exponent", [127, 120, 0, -60, -90])
 def test_bf16_values_of_any_size(exponent, d, lens):
