@@ -20,9 +20,10 @@ namespace tq {
 
 namespace {
 
-// sums past these are formed again of scaled values: the largest values' squares pass fp32's
-// range, the smallest ones' vanish
-constexpr float kMost = 0x1p126f, kLeast = 0x1p-100f, kDown = 0x1p-70f, kUp = 0x1p60f;
+// Sums past these are formed again of scaled values: the largest values' squares pass fp32's
+// range, the smallest ones' vanish.  (Down: 32768 values of 2^128 sum up to 2^(2 (128 - 80) + 15)
+// = 2^111; a row whose sum passed 2^126 has a mean of 2^(111 - 160) or more.)
+constexpr float kMost = 0x1p126f, kLeast = 0x1p-100f, kDown = 0x1p-80f, kUp = 0x1p60f;
 
 template <bool BF16>
 __device__ __forceinline__ void unpack8(u32x4 w, float (&f)[8]) {
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
     if (again) {
       by = sum < 1.0f ? kUp : kDown;
       sum = squares(f, by);
-      eps *= by * by;
+      eps = eps * by * by;       // (by * by may vanish)
     }
     return by / sqrtf(fmaf(sum, inv_n, eps));
   };

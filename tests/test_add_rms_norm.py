@@ -193,3 +193,24 @@ def test_other_stream_and_graph(tokens, n):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@gpu
+@pytest.mark.parametrize("n", [8, 4096, 8192, 32768])
+def test_largest_values(n):
+    """Rows of bf16's largest values, whose squares' sum passes fp32's range also of values scaled by 2^-70."""
+    say("largest", n)
+    sign = torch.where(randn(3, n, seed=1) > 0, 1.0, -1.0).double()
+    w = (1 + 0.2 * randn(n, seed=3)).to(BF16)
+    for x in (sign * torch.finfo(BF16).max, sign * 2.0 ** 127 * (1 + 0.9 * torch.rand(3, n, generator=torch.Generator().manual_seed(2)))):
+        x = x.clamp(-torch.finfo(BF16).max, torch.finfo(BF16).max).to(BF16)
+        held(x, None, w, eps=0.0)
+        held(x, None, w, eps=1e-6)
+        # the norm after a block; the norm of a residual sum
+        held(x, randn(3, n, seed=4).to(BF16), w, w)
+        y = tq.add_rms_norm((0.4 * x.double()).to(BF16).cuda(), (0.5 * x.double()).to(BF16).cuda(), w.cuda(), return_sum=False)
+        _, _, want, off = plain((0.4 * x.double()).to(BF16), (0.5 * x.double()).to(BF16), w, None, None, 1.0, 1e-6)
+        assert bool(((y.cpu().double() - want).abs() <= ulp(BF16) * want.abs() * (1 + 2.0 ** -10) + 2 * off).all())
+    # an eps as large as a mean whose sum is just past the range
+    for eps in (1e33, 1e36, 3e38):
+        held((x.double() * 2.0 ** -71).to(BF16), None, w, eps=eps)
