@@ -22,8 +22,9 @@ namespace {
 
 // Sums past these are formed again of scaled values: the largest values' squares pass fp32's
 // range, the smallest ones' vanish.  (Down: 32768 values of 2^128 sum up to 2^(2 (128 - 80) + 15)
-// = 2^111; a row whose sum passed 2^126 has a mean of 2^(111 - 160) or more.)
-constexpr float kMost = 0x1p126f, kLeast = 0x1p-100f, kDown = 0x1p-80f, kUp = 0x1p60f;
+// = 2^111; a row whose sum passed 2^126 has a mean of 2^(111 - 160) or more.  Up: a sum below
+// 2^(15 - 100) ends below 2^115, and fp32's smallest value at 2^(2 (100 - 149)) = 2^-98.)
+constexpr float kMost = 0x1p126f, kLeast = 0x1p-100f, kDown = 0x1p-80f, kUp = 0x1p100f;
 
 template <bool BF16>
 __device__ __forceinline__ void unpack8(u32x4 w, float (&f)[8]) {
@@ -78,16 +79,23 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
       }
     return row_sum(v);
   };
-  // 1 / sqrt(mean(f^2) + eps)
+  // 1 / sqrt(mean(f^2) + eps).  (Of a row of small values, whose factor may pass fp32's range: of
+  // the row times a power of two, which f then is.)
   const float inv_n = 1.0f / (float)a.n;
-  auto inverse = [&](const float (&f)[C][8]) -> float {
+  auto inverse = [&](float (&f)[C][8]) -> float {
     float sum = squares(f, 1.0f), by = 1.0f, eps = a.eps;
-    const bool again = !(sum <= kMost) || fmaf(sum, inv_n, eps) < kLeast;
     // (the threads of a row agree; where a row is a wavefront's, wavefronts need not)
-    if (again) {
-      by = sum < 1.0f ? kUp : kDown;
+    if (!(sum <= kMost)) {
+      by = kDown;
       sum = squares(f, by);
       eps = eps * by * by;       // (by * by may vanish)
+    } else if (fmaf(sum, inv_n, eps) < kLeast) {
+#pragma unroll
+      for (int c = 0; c < C; c++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[c][i] *= kUp;
+      sum = squares(f, 1.0f);
+      eps = eps * kUp * kUp;
     }
     return by / sqrtf(fmaf(sum, inv_n, eps));
   };

@@ -214,3 +214,18 @@ def test_largest_values(n):
     # an eps as large as a mean whose sum is just past the range
     for eps in (1e33, 1e36, 3e38):
         held((x.double() * 2.0 ** -71).to(BF16), None, w, eps=eps)
+
+
+@gpu
+@pytest.mark.parametrize("n", [8, 4096, 32768])
+@pytest.mark.parametrize("exponent", [-126, -129, -133])
+def test_smallest_values(n, exponent):
+    """Rows down to bf16's smallest values, normed without eps: the factor itself passes fp32's range."""
+    say("smallest", n, exponent)
+    sign = torch.where(randn(3, n, seed=1) > 0, 1.0, -1.0).double()
+    w = (1 + 0.2 * randn(n, seed=3)).to(BF16)
+    x = (sign * 2.0 ** exponent * torch.randint(1, 4, (3, n), generator=torch.Generator().manual_seed(2))).to(BF16)
+    held(x, None, w, eps=0.0)
+    held(x, randn(3, n, seed=4).to(BF16), w, w, eps=0.0)
+    held(x, None, w, eps=1e-6)
+    held(x, None, w, eps=2.0 ** -140)
