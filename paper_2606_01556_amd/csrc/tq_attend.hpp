@@ -388,7 +388,8 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     float m = -FLT_MAX, l = 0.0f;
     float most = kTopWeight, headroom = kHeadroom;
     if constexpr (VBF) {
-      const int e = 32 - __builtin_clz(rg.len);
+      // (parts that a prefix's are added to: half the range each)
+      const int e = 32 - __builtin_clz(rg.len) + (parts_only ? 1 : 0);
       most = __builtin_bit_cast(float, (127 - e) << 23);
       headroom = (float)(-e - kBelow);
     }

@@ -276,7 +276,8 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   // binades above the reference at which it has to move, and where it puts the largest weight
   float most = kTopBinades, headroom = kHeadroom;
   if constexpr (VBF) {
-    most = (float)(__builtin_clz(max(len, 1)) - 32);
+    // (a shared prefix: its sums are added to those of a stream's own keys, half the range each)
+    most = (float)(__builtin_clz(max(len, 1)) - 32 - (a.shared ? 1 : 0));
     headroom = most - kBelow;
   }
 

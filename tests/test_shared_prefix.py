@@ -242,3 +242,45 @@ def test_shared_prefix_other_stream_and_graph():
         torch.cuda.synchronize()
         for g, out in graphs:
             assert torch.equal(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_shared_prefix_of_the_largest_values(d):
+    """bf16's largest value everywhere, and weights as large as either half of a row holds them: keys
+    just less than 8 binades above the first 32 of each part, which set its reference."""
+    say("largest", d)
+    n = 511
+    s = Shared([n], [0, 1], [n], 1, d, 16, "bf16", BF16)
+    every = torch.cat(s.slots).cuda()
+    k, v = torch.zeros(2 * n, 1, d), torch.full((2 * n, 1, d), torch.finfo(BF16).max)
+    k[:n, 0, 0] = torch.where((torch.arange(n) % 256) < 32, 0.0, 5.46875)     # (parts of 256 keys)
+    k[n:, 0, 0] = torch.where(torch.arange(n) < 256, 0.0, 5.46875)            # (eight wavefronts' first steps)
+    tq.kv_append(s.cache, k.to(BF16).cuda(), v.to(BF16).cuda(), every)
+    q = torch.zeros(1, 1, d)
+    q[..., 0] = d ** 0.5
+    for exact in (False, True):
+        for scale in (d ** -0.5, 0.0):
+            got = s.call(q.to(BF16), scale=scale, exact=exact)
+            assert bool((got == torch.finfo(BF16).max).all()), got.flatten()[:4]
+
+
+@gpu
+@pytest.mark.parametrize("exponent", [127, 120, 0, -60, -90])
+@pytest.mark.parametrize("shape", [0, 2, 3])
+def test_shared_prefix_bf16_values_of_any_size(exponent, shape, monkeypatch):
+    say("range", exponent, shape)
+    s = Shared(*SHARED[shape], 1, 64, 16, "bf16", BF16)
+    total = sum(s.lens)
+    v = torch.where(randn(total, 1, 64, seed=3) > 0, 1.0, -1.0) * (1.0 + 0.99 * torch.rand(total, 1, 64, generator=torch.Generator().manual_seed(4)))
+    v = (v.double() * 2.0 ** exponent).clamp(-torch.finfo(BF16).max, torch.finfo(BF16).max).to(BF16)
+    every = torch.cat(s.slots).cuda()
+    k, _ = tq.kv_read(s.cache, every)
+    tq.kv_append(s.cache, k, v.cuda(), every)
+    s.v = v.double().numpy()
+    q = (1.3 * randn(len(s.own), 4, 64, seed=9)).to(BF16)
+    got = s.call(q).cpu().double().numpy()
+    monkeypatch.setattr(Prompts, "floor", 2.0 ** -133)
+    ref, _, bound, _ = s.plain(q, 64 ** -0.5)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - ref) <= bound).all()
