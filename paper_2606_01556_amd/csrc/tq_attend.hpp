@@ -184,9 +184,9 @@ __device__ __forceinline__ void store4(const AttendArgs &a, int d, int64_t row, 
     a.lse[row] = (m + (float)__builtin_amdgcn_frexp_expf(l) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l))) * (1.0f / kLog2e);
 }
 
-// The parts' slots: two of every run; where whole ranges leave parts too, one of every range
-// behind them.
-__host__ __device__ constexpr int64_t part_slots(int64_t blocks, int64_t ranges) { return 2 * blocks + ranges; }
+// The parts' slots: two of every run (none where work-groups hold one range each); where whole
+// ranges leave parts too, one of every range behind them.
+__host__ __device__ constexpr int64_t run_slots(int64_t blocks, bool direct) { return direct ? 0 : 2 * blocks; }
 
 // What the first launch tells the join about a range, [batch][vheads]: the number
 // of its first part and of its parts (0: nothing to join).  Part 2 w is the first
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
   }
   float *const parts = a.scratch;
   const bool parts_only = SCORED && a.parts;
-  Join *const joins = reinterpret_cast<Join *>(a.scratch + part_slots(gridDim.x, parts_only ? (int64_t)a.batch * vheads : 0) * part_floats(D, cols));
+  Join *const joins = reinterpret_cast<Join *>(a.scratch + (run_slots(gridDim.x, DIRECT) + (parts_only ? (int64_t)a.batch * vheads : 0)) * part_floats(D, cols));
   // streams that hold nothing
   auto clear = [&](int64_t row0, int rows) {
     for (int e = threadIdx.x; e < rows * (D / 2); e += 64 * W) reinterpret_cast<uint32_t *>(a.out + row0 * D)[e] = 0;
@@ -653,7 +653,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     const bool all = n == rg.steps, whole = all && !parts_only;
     const int64_t row0 = (int64_t)b * a.hq + kvh * a.group + h0;
     int slot = 2 * blockIdx.x + (x == x0 ? 0 : 1);
-    if (parts_only && all) slot = 2 * (int)gridDim.x + b * vheads + vh;
+    if (parts_only && all) slot = (int)run_slots(gridDim.x, DIRECT) + b * vheads + vh;
     float *part = parts + (int64_t)slot * part_floats(D, cols);
     if ((!DIRECT || parts_only) && t == 0 && threadIdx.x == 0) {
       const int end = x + rg.steps - 1;      // the range's last step
@@ -707,7 +707,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttendArgs a) 
   __shared__ __attribute__((aligned(16))) float lds_o[GROUPS][D], lds_ml[GROUPS][2];
   const int b = blockIdx.y, vh = blockIdx.x, vheads = gridDim.x;
   const int hr = kHeads * head_blocks(a.group), hblocks = (a.group + hr - 1) / hr, cols = min(a.group, hr);
-  const Join *joins = reinterpret_cast<const Join *>(a.scratch + part_slots(a.blocks, 0) * part_floats(D, cols));
+  const Join *joins = reinterpret_cast<const Join *>(a.scratch + run_slots(a.blocks, false) * part_floats(D, cols));
   const Join j = joins[(int64_t)b * vheads + vh];
   if (j.parts == 0) return;                      // written by its work-group
   const int kvh = vh / hblocks, h0 = vh % hblocks * hr;

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_prefix_kernel(const PrefixA
     const int hr = kHeads * head_blocks(t.group), cols = min(t.group, hr), ranges = (t.group + hr - 1) / hr;
     const int kvh = h / t.group, in = h - kvh * t.group, place = in % hr;
     const int64_t all = (int64_t)t.batch * p.c.heads * ranges;
-    const Join j = reinterpret_cast<const Join *>(t.scratch + part_slots(t.blocks, all) * part_floats(D, cols))[
+    const Join j = reinterpret_cast<const Join *>(t.scratch + (run_slots(t.blocks, t.direct) + all) * part_floats(D, cols))[
         ((int64_t)stream * p.c.heads + kvh) * ranges + in / hr];
     const float *const parts = p.scratch + parts_head(p.splits, heads);
 #pragma unroll 4
@@ -92,7 +92,7 @@ hipError_t join_prefix(const PrefixArgs &a, bool bf16, hipStream_t s) {
 size_t attend_parts_bytes(const KvCache &c, int batch, int hq, const AttendPlan &p) {
   const int group = hq / c.heads;
   const int64_t ranges = (int64_t)batch * c.heads * ranges_of(group);
-  return (size_t)part_slots(p.blocks, ranges) * part_floats(c.d, range_heads(group)) * sizeof(float) + (size_t)ranges * sizeof(Join);
+  return (size_t)(run_slots(p.blocks, p.direct) + ranges) * part_floats(c.d, range_heads(group)) * sizeof(float) + (size_t)ranges * sizeof(Join);
 }
 
 hipError_t launch_prefix(const PrefixArgs &a, bool bf16, hipStream_t s) {

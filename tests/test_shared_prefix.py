@@ -284,3 +284,14 @@ def test_shared_prefix_bf16_values_of_any_size(exponent, shape, monkeypatch):
     ref, _, bound, _ = s.plain(q, 64 ** -0.5)
     assert np.isfinite(got).all()
     assert (np.abs(got - ref) <= bound).all()
+
+
+def test_shared_prefix_scratch_is_what_the_parts_take():
+    """Short own ranges are one part each."""
+    L = tq.lib()
+    for batch, heads, group, d, pages in ((1024, 8, 32, 256, 1), (512, 8, 4, 128, 2), (3, 1, 1, 64, 1)):
+        hq = heads * group
+        got = L.tq_shared_prefix_attention_scratch_bytes(desc(kv_heads=heads, head_dim=d, page_size=16), batch, hq, 1, 1, pages)
+        most = 4 * batch * hq * (d + 2) + 256                                  # the prefix's
+        most += 4 * batch * heads * (group * (d + 2) + 4) + 8 * batch * heads   # the streams' and where they are
+        assert 0 < got <= most, (got, most)
