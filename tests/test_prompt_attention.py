@@ -569,3 +569,18 @@ def test_scales_that_are_not_finite(kind, dtype, lens, new):
                     # (the same sum from another reference, as in test_values_that_are_no_number)
                     assert bool(((got_lse - lse).abs() <= 2.0 ** -16 * (1 + lse.abs())).all())
                 scales.copy_(keep)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_streams_in_another_order(kind, dtype):
+    """What a row gets does not depend on where in the call its stream stands."""
+    say("order", kind, dtype)
+    s, q = prompts([500, 420, 9], [500, 400, 9], 2, 4, 128, 16, kind, dtype)
+    ref, lse = s.call(q, return_lse=True)
+    table, lengths = s.args()
+    order = [2, 0, 1]
+    rows = np.concatenate([np.arange(s.starts[i], s.starts[i + 1]) for i in order])
+    starts = torch.tensor(np.cumsum([0] + [s.new[i] for i in order]), dtype=torch.int32).cuda()
+    got, got_lse = tq.prompt_attention(s.cache, q[rows].cuda(), starts, table[order].contiguous(), lengths[order].contiguous(), return_lse=True)
+    assert torch.equal(got, ref[rows]) and torch.equal(got_lse, lse[rows])

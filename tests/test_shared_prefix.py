@@ -286,6 +286,53 @@ def test_shared_prefix_bf16_values_of_any_size(exponent, shape, monkeypatch):
     assert (np.abs(got - ref) <= bound).all()
 
 
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_shared_prefix_values_that_are_no_number(kind, dtype):
+    """A value that is not finite shows in its channels of the streams that see it, and nowhere else;
+    what lies behind a prefix's or a stream's end has no part."""
+    say("no number", kind, dtype)
+    s = Shared([100, 300], [0, 2, 4], [3, 70, 0, 20], 2, 128, 16, kind, dtype)
+    q = randn(5, 8, 128, seed=1).to(dtype)
+    table, lengths = s.args()
+    extra = table[2:3], lengths[2:3]               # a stream of no group, of the first one's own tokens
+    m = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    call = lambda: tq.shared_prefix_attention(s.cache, q.cuda(), m, table[:2], lengths[:2], torch.cat((table[2:], extra[0])),
+                                              torch.cat((lengths[2:], extra[1])), return_lse=True)
+    ref, lse = call()
+    bits, page = s.cache.bits, s.cache.page_size
+    # (a prefix or a stream's own tokens, one of its keys, and the streams that see it)
+    for which, key, sees in ((0, 50, [0, 1]), (1, 299, [2, 3]), (3, 69, [1]), (2, 0, [0, 4])):
+        slot = int(s.slots[which][key])
+        for value in (math.nan, math.inf):
+            rows = s.cache.v if bits == 16 else s.cache.v_scales
+            keep = rows.clone()
+            at = (slot // page, 1, slot % page) + ((5,) if bits == 16 else ())
+            rows[at] = value
+            got, got_lse = call()
+            hit = np.zeros((5, 8, 128), bool)
+            hit[np.ix_(sees, [4, 5, 6, 7], [5] if bits == 16 else np.arange(128))] = True
+            np.testing.assert_array_equal(torch.isfinite(got.float()).cpu().numpy(), ~hit)
+            other = [i for i in range(5) if i not in sees]
+            assert torch.equal(got[other], ref[other]) and torch.equal(got_lse[other], lse[other])
+            rows.copy_(keep)
+
+
+@gpu
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("page", [128, 1024])
+def test_shared_prefix_many_groups_and_large_pages(kind, dtype, page):
+    """More groups than a search step looks at, some of them empty, some without a prefix."""
+    say("groups", kind, dtype, page)
+    rng = np.random.default_rng(0)
+    sizes = [int(x) for x in rng.choice([0, 0, 1, 2, 3], 150)]
+    shared = [int(x) for x in rng.choice([0, 1, 40, 130, 200], 150)]
+    s = Shared(shared, np.concatenate(([0], np.cumsum(sizes))), [int(x) for x in rng.choice([0, 1, 30, 70], sum(sizes) + 3)], 1, 64, page,
+               kind, dtype)
+    q = (1.3 * randn(len(s.own), 4, 64, seed=9)).to(dtype)
+    check(*s.call(q, return_lse=True), *s.plain(q, 64 ** -0.5))
+
+
 def test_shared_prefix_scratch_is_what_the_parts_take():
     """Short own ranges are one part each."""
     L = tq.lib()
