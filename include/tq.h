@@ -438,7 +438,8 @@ typedef struct {
 
 /* tq_paged_attention with such scores, the token at position lengths[i] - 1 (its scratch
  * size is tq_paged_attention_scratch_bytes).  With softcap 0 and no slopes it is
- * tq_paged_attention.  The tanh is good to 2^-22 of the cap.
+ * tq_paged_attention.  A capped score is good to 2^-21 of the cap, and to 2^-20 of itself where
+ * the cap is above 64.
  * Errors as tq_paged_attention; TQ_ERR_SHAPE for a softcap that is negative or not finite. */
 tq_status tq_paged_attention_scored(const tq_kv_cache *c, const tq_head_rows *q, tq_dtype dtype, int batch,
                                     int q_heads, const int32_t *page_table, int64_t table_stride,

@@ -365,7 +365,7 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
     const float c0 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f) * (SK ? kSmall : 1.0f);  // (-infinity times it has to stay so)
     // (scored: in binades before the softmax)
     const float c1 = SCORED ? 1.0f : c0;
-    const Shape shape = SCORED ? shape_of(a.scale, a.cap, SK ? kSmall : 1.0f) : Shape{};
+    const Shape shape = SCORED ? shape_of(a.scale, a.cap, c0, SK ? kSmall : 1.0f) : Shape{};
     const float slope = SCORED && a.slopes != nullptr ? a.slopes[kvh * a.group + h0 + min(wb * kHeads + r, a.group - h0 - 1)] * kLog2e : 0.0f;
     {
       const uint16_t *qp = a.q + b * a.q_ts + (int64_t)(kvh * a.group + h0 + min(wb * kHeads + r, a.group - h0 - 1)) * a.q_hs;
@@ -427,11 +427,21 @@ __global__ __launch_bounds__(64 * W, W == kDirectWaves ? 2 : runs_per_cu(D)) voi
 #pragma unroll
         for (int j = 0; j < 4; j++) s[i][j] = BITS < 16 ? fmaf(acc[i][j], scale_of(ksr[i], j), 0.0f) : acc[i][j];
       if constexpr (SCORED) {
+        if (a.cap > 0.0f) {
+          auto at = [&](int v) -> float { return s[v / 4][v % 4]; };
+          auto set = [&](int v, float y) { s[v / 4][v % 4] = y; };
+          if (a.cap > kWide) cap_scores<4 * NT, true>(at, set, shape);
+          else cap_scores<4 * NT, false>(at, set, shape);
+        } else {
+#pragma unroll
+          for (int i = 0; i < NT; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) s[i][j] *= c0;
+        }
 #pragma unroll
         for (int i = 0; i < NT; i++)
 #pragma unroll
           for (int j = 0; j < 4; j++) {
-            s[i][j] = a.cap > 0.0f ? capped(s[i][j], shape) : s[i][j] * c0;
             if (a.slopes != nullptr) s[i][j] = fmaf(-slope, fabsf((float)(rg.len - 1 - (t0 + 16 * i + 4 * g + j))), s[i][j]);
           }
       }

@@ -120,13 +120,18 @@ struct Interval {
   int lo, hi;
 };
 
-template <int D, int BITS, bool BF16, bool EXT, bool FINE>
+// How a score is made of its product: by a factor alone; capped or biased; with a cap past 64, whose
+// two ways would cost the others registers (16 / 4 heads of 64: 97 us for 86).
+enum Scored { kPlain, kCapped, kCappedWide };
+
+template <int D, int BITS, bool BF16, Scored HOW, bool FINE>
 __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void prompt_kernel(const PromptArgs a) {
   constexpr int KT = kTileKeys, W = kPromptWaves, T = kPromptThreads;
   constexpr int RB = D * BITS / 8;              // bytes of a cache row
   constexpr int LB = D * 2, LC = LB / 16;       // bytes and 16-byte pieces of a row in LDS
   constexpr int KS = D / 16, DT = D / 32;
   constexpr bool VBF = BITS == 16 && BF16;      // type of the second product
+  constexpr bool EXT = HOW != kPlain;
   constexpr int TB = KT * LB;                   // bytes of a tile in LDS
   constexpr auto key_tile = [](int odd) { return odd * TB; };
   constexpr auto value_tile = [](int odd) { return (2 + odd) * TB; };
@@ -271,7 +276,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
 
   // what a score's product with the key's scale is multiplied by, in binades
   const float c1 = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-149f);     // (-infinity times it has to stay so)
-  const Shape shape = EXT ? shape_of(a.scale, a.cap, 1.0f) : Shape{};
+  const Shape shape = EXT ? shape_of(a.scale, a.cap, c1, 1.0f) : Shape{};
   const float slope = EXT && a.slopes != nullptr ? a.slopes[head] * kLog2e : 0.0f;
   // binades above the reference at which it has to move, and where it puts the largest weight
   float most = kTopBinades, headroom = kHeadroom;
@@ -403,8 +408,7 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   auto refer = [&](v16f &sc, int k, int i, uint32_t vscales, auto edge) __attribute__((always_inline)) {
     if constexpr (EXT) {
       if (a.cap > 0.0f) {
-#pragma unroll
-        for (int v = 0; v < 16; v++) sc[v] = capped(sc[v], shape);
+        cap_scores<16, HOW == kCappedWide>([&](int v) -> float { return sc[v]; }, [&](int v, float y) { sc[v] = y; }, shape);
       } else {
 #pragma unroll
         for (int v = 0; v < 16; v++) sc[v] *= c1;
@@ -683,12 +687,12 @@ __global__ __launch_bounds__(kPromptThreads, prompt_occupancy(D, BITS)) void pro
   }
 }
 
-template <int D, int BITS, bool BF16, bool EXT, bool FINE>
+template <int D, int BITS, bool BF16, Scored HOW, bool FINE>
 hipError_t go_prompt(const PromptArgs &a, hipStream_t s) {
   const int bytes = prompt_lds_bytes(D, BITS);
-  const hipError_t e = allow_lds(reinterpret_cast<const void *>(prompt_kernel<D, BITS, BF16, EXT, FINE>), bytes);
+  const hipError_t e = allow_lds(reinterpret_cast<const void *>(prompt_kernel<D, BITS, BF16, HOW, FINE>), bytes);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((prompt_kernel<D, BITS, BF16, EXT, FINE>), dim3((uint32_t)a.blocks), dim3(kPromptThreads), bytes, s, a);
+  hipLaunchKernelGGL((prompt_kernel<D, BITS, BF16, HOW, FINE>), dim3((uint32_t)a.blocks), dim3(kPromptThreads), bytes, s, a);
   return hipGetLastError();
 }
 
@@ -699,13 +703,17 @@ template <int D>
 hipError_t launch_prompt_d(const PromptArgs &a, bool bf16, hipStream_t s) {
   typedef std::true_type Yes;
   typedef std::false_type No;
-  const bool ext = a.cap > 0.0f || a.slopes != nullptr;
-  auto go = [&](auto bits, auto b, auto e) -> hipError_t {
+  auto go = [&](auto bits, auto b, auto how) -> hipError_t {
     constexpr int BITS = decltype(bits)::value;
-    constexpr bool BF16 = decltype(b)::value, EXT = decltype(e)::value;
-    return a.fine ? go_prompt<D, BITS, BF16, EXT, true>(a, s) : go_prompt<D, BITS, BF16, EXT, false>(a, s);
+    constexpr bool BF16 = decltype(b)::value;
+    constexpr Scored HOW = decltype(how)::value;
+    return a.fine ? go_prompt<D, BITS, BF16, HOW, true>(a, s) : go_prompt<D, BITS, BF16, HOW, false>(a, s);
   };
-  auto go_ext = [&](auto bits, auto b) -> hipError_t { return ext ? go(bits, b, Yes()) : go(bits, b, No()); };
+  auto go_ext = [&](auto bits, auto b) -> hipError_t {
+    if (a.cap > kWide) return go(bits, b, std::integral_constant<Scored, kCappedWide>());
+    if (a.cap > 0.0f || a.slopes != nullptr) return go(bits, b, std::integral_constant<Scored, kCapped>());
+    return go(bits, b, std::integral_constant<Scored, kPlain>());
+  };
   auto go_type = [&](auto bits) -> hipError_t { return bf16 ? go_ext(bits, Yes()) : go_ext(bits, No()); };
   if (a.c.bits == 16) return go_type(std::integral_constant<int, 16>());
   if (a.c.bits == 8) return go_type(std::integral_constant<int, 8>());
