@@ -26,7 +26,10 @@ constexpr int kScale2p9 = 127 + 9;  // E8M0 block scale 2^9
 // Direct loads of 16 bytes per lane into LDS at lds + 16 * lane, from a scalar base and a 32-bit
 // lane offset or from an address per lane.  (The s_nop: a scalar write of m0 needs one wait
 // state before such a load reads it, which the hardware does not insert, nor the compiler
-// within an asm string.)
+// within an asm string.  m0 is no register that the compiler allocates, but it may count on what
+// it wrote there.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(uint32_t voff, const uint8_t *sbase, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "s"(lds)
                : "memory", "m0");
@@ -34,6 +37,7 @@ __device__ __forceinline__ void load_to_lds(uint32_t voff, const uint8_t *sbase,
 __device__ __forceinline__ void load_to_lds(const uint8_t *addr, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // TQ4 word -> two words of fp8 e4m3 bytes (codes 0..3 and 4..7, in order).
 __device__ __forceinline__ void tq4_to_fp8(uint32_t w, uint32_t &lo, uint32_t &hi) {
