@@ -79,25 +79,25 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
       }
     return row_sum(v);
   };
-  // 1 / sqrt(mean(f^2) + eps).  (Of a row of small values, whose factor may pass fp32's range: of
-  // the row times a power of two, which f then is.)
+  // 1 / sqrt(mean(f^2) + eps) as up * inv: of a row of small values it may pass fp32's range
+  struct Inverse {
+    float up, inv;
+  };
   const float inv_n = 1.0f / (float)a.n;
-  auto inverse = [&](float (&f)[C][8]) -> float {
-    float sum = squares(f, 1.0f), by = 1.0f, eps = a.eps;
+  auto inverse = [&](const float (&f)[C][8]) -> Inverse {
+    float sum = squares(f, 1.0f), by = 1.0f, up = 1.0f, eps = a.eps;
+    const bool again = !(sum <= kMost) || fmaf(sum, inv_n, eps) < kLeast;
     // (the threads of a row agree; where a row is a wavefront's, wavefronts need not)
-    if (!(sum <= kMost)) {
-      by = kDown;
+    if (again) {
+      by = sum < 1.0f ? kUp : kDown;
       sum = squares(f, by);
-      eps = eps * by * by;       // (by * by may vanish)
-    } else if (fmaf(sum, inv_n, eps) < kLeast) {
-#pragma unroll
-      for (int c = 0; c < C; c++)
-#pragma unroll
-        for (int i = 0; i < 8; i++) f[c][i] *= kUp;
-      sum = squares(f, 1.0f);
-      eps = eps * kUp * kUp;
+      eps = eps * by * by;       // (by * by may vanish, or pass the range)
+      if (by > 1.0f) {
+        up = by;
+        by = 1.0f;
+      }
     }
-    return by / sqrtf(fmaf(sum, inv_n, eps));
+    return {up, by / sqrtf(fmaf(sum, inv_n, eps))};
   };
 
   float x[C][8], s[C][8], gate[C][8];
@@ -114,14 +114,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
     }
   }
   if (a.post != nullptr) {
-    const float inv = inverse(x);
+    const Inverse i1 = inverse(x);
 #pragma unroll
     for (int c = 0; c < C; c++) {
       const int p = c * T + t;
       float w[8];
       unpack8<BF16>(*reinterpret_cast<const u32x4 *>(a.post + 8 * min(p, pieces - 1)), w);
 #pragma unroll
-      for (int i = 0; i < 8; i++) x[c][i] = x[c][i] * inv * w[i];
+      for (int i = 0; i < 8; i++) x[c][i] = x[c][i] * i1.up * i1.inv * w[i];
     }
   }
 #pragma unroll
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
     if (c * T + t >= pieces)
 #pragma unroll
       for (int i = 0; i < 8; i++) s[c][i] = 0.0f;
-  const float inv = inverse(s);
+  const Inverse i2 = inverse(s);
 #pragma unroll
   for (int c = 0; c < C; c++) {
     const int p = c * T + t;
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(const NormArgs 
       float w[8];
       unpack8<BF16>(*reinterpret_cast<const u32x4 *>(a.weight + 8 * p), w);
 #pragma unroll
-      for (int i = 0; i < 8; i++) w[i] = s[c][i] * inv * w[i];
+      for (int i = 0; i < 8; i++) w[i] = s[c][i] * i2.up * i2.inv * w[i];
       *reinterpret_cast<u32x4 *>(a.normed + row * a.n + 8 * p) = pack8<BF16>(w);
     }
   }
