@@ -428,7 +428,7 @@ tq_status tq_paged_attention(const tq_kv_cache *c, const tq_head_rows *q, tq_dty
  *   slopes != NULL: s -= slopes[query head] * |p - j|  (fp32 [q_heads]).
  * window > 0: only keys j > p - window.
  * exact: the softmax's weights enter the product with v as two 16-bit terms, 22 bits (16-bit
- * cache of bf16 values: 16), and not rounded once; about 30 % more time where the products
+ * cache of bf16 values: 16), and not rounded once; about a third more time where the products
  * bound it.  (tq_paged_attention holds that much in any case.) */
 typedef struct {
     float scale, softcap;

@@ -39,15 +39,20 @@
 //
 // Measured, where the products are the bound (PyTorch's bf16 product of two 8192 x 8192 matrices
 // reaches 1.22 to 1.27 PFLOP/s on the same card):
-//   1 prompt of 8192 tokens, 32 / 8 heads of 128, fp16          560 us, 982 TFLOP/s (exact: 740)
-//   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2530 us, 842 TFLOP/s
-//   2 prompts of 4096, 16 / 8 heads of 256, window 1024, capped 191 us, 520 TFLOP/s
+//   1 prompt of 8192 tokens, 32 / 8 heads of 128, fp16          561 us, 980 TFLOP/s (exact: 764, 719)
+//   2048 tokens behind 30720, 64 / 8 heads of 128, 8 bits      2500 us, 852 TFLOP/s (exact: 3336, 639)
+//   2 prompts of 4096, 16 / 8 heads of 256, window 1024, capped 192 us, 518 TFLOP/s (exact: 217, 456)
+// (another card of the kind: 624, 2796 and 194 us)
 // The matrix cores are busy half of the first's cycles, without bank conflicts, and the clock is
 // at 1.9 GHz of 2.4: as steps took cycles away (1.38 million at first, 1.07 now) it went down
 // from 2.05.  Left out one at a time (in a copy), the loads give 75 us back, the exponentials 45,
 // the maxima 40, half of the second products 58: no single one holds the others up.  With keys a
 // whole tile ahead the first takes 548 us, but codes spill registers (8 bits 4100 to 7100 us) and
 // 32 prompts up to 700 take 134 us for 121; with none ahead 569, and 215 for the 191.
+//
+// Registers that the kernels spill as they are: head_dim 128 at 8 bits 8 (exact 19, capped or biased
+// 34 to 37), at 4 bits none (exact 5, capped or biased 14 to 23), at 16 bits none (capped or biased 5
+// to 8); head_dim 64 at 16 bits, capped or biased, 8 to 15, where three wavefronts a SIMD leave 168.
 #pragma once
 
 #include <cfloat>

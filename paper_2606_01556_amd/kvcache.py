@@ -290,7 +290,7 @@ def prompt_attention(cache: KVCache, q, starts, page_table, lengths, scale: floa
     > 0: scores s become softcap * tanh(s / softcap); slopes [q_heads] float32: less
     slopes[h] times the distance.  scale: head_dim^-1/2 by default.  The softmax's weights
     enter the product with v rounded to 16 bits; exact: with 22 bits (16-bit cache of
-    bfloat16: 16) as in ``paged_attention``, in about 30 % more time, for a token's result
+    bfloat16: 16) as in ``paged_attention``, in up to 35 % more time, for a token's result
     not to depend on whether it came in a prompt or alone by more than its last rounding.
 
     Returns out [tokens, q_heads, head_dim] of q's type, zeros for a token that sees
